@@ -77,7 +77,8 @@ enum {
     CONFU_ST_BAD_PLAN = 10       /* confu_tree_attention: the plan was built for another attention path */
 };
 
-enum { CONFU_BF16 = 0, CONFU_F32 = 1, CONFU_FP8_E4M3 = 2 };   /* FP8: cache entries only, see confu_set_kv_scales */
+enum { CONFU_BF16 = 0, CONFU_F32 = 1, CONFU_FP8_E4M3 = 2,    /* FP8: cache entries only, see confu_set_kv_scales */
+       CONFU_FP8_BLOCK = 3 };                                 /* the same with a scale per block, see confu_set_kv_block_scales */
 
 #define CONFU_MAX_TREE  64      /* T: tree rows (one 64-bit ancestor word per row) */
 #define CONFU_MAX_ROWS  128     /* R = T + C, with C <= 64: covers one contemplate row per node (R = 2T) */
@@ -91,7 +92,7 @@ typedef struct {
     int32_t T, C;       /* tree rows (root included), contemplate rows */
     int32_t S;          /* soft-prompt KV entries, shared by all sequences (0 allowed) */
     int32_t kv_dtype;   /* CONFU_BF16 | CONFU_F32: type of q, caches, soft KV and out;
-                           CONFU_FP8_E4M3: caches and soft KV are E4M3 bytes, q and out are bf16 */
+                           CONFU_FP8_E4M3, CONFU_FP8_BLOCK: caches and soft KV are E4M3 bytes, q and out are bf16 */
     float   sm_scale;   /* 0 -> D^-1/2 */
 } confu_dims;
 
@@ -135,7 +136,8 @@ int confu_set_paging(confu_ctx* ctx, const int32_t* block_table, int32_t max_pag
  *                             it before confu_tree_plan: a plan only fits the path it was built
  *                             for (status CONFU_ST_BAD_PLAN otherwise), as confu_attention_path names it.  For small
  *                             batches _AUTO takes a form of its own of _TENSOR, _TENSOR_NARROW (one
- *                             M tile of query rows per CTA), which cannot be set.
+ *                             M tile of query rows per CTA), which cannot be set.  For CONFU_FP8_BLOCK _GENERIC is the kernel that
+ *                             keeps keys and values in registers (every supported shape).
  *   CONFU_OPT_WAIT_LIMIT_NS   wall-clock limit of every wait on a barrier inside the tensor-core
  *                             kernels (default 2 s; 1 us .. 10 s).  A wait that runs out makes the
  *                             kernel release what it holds and report CONFU_ST_TIMEOUT.
@@ -177,6 +179,30 @@ int confu_selftest_bounded_wait(confu_ctx* ctx, int64_t limit_ns, int32_t* statu
  *   - confu_kv_compact moves bytes as for any other type.
  */
 int confu_set_kv_scales(confu_ctx* ctx, const float* k_scale, const float* v_scale);
+
+/*
+ * 8-bit caches with a scale for each block of tokens and head (kv_dtype = CONFU_FP8_BLOCK; the paper has no cache
+ * format).  Entries are E4M3 bytes as above, in paged pools (confu_set_paging; CONFU_ERR_UNSUPPORTED without a block table); an
+ * entry stands for  code * scale  of its block: k_scale, v_scale are DEVICE fp32 arrays [pages][Hkv][128 / block] of the
+ * layer, block (32, 64 or 128 tokens) the run of slots within a page that shares a scale.  They are positive and finite
+ * wherever a block holds an entry of a sequence, and are not interpreted elsewhere.  The soft-prompt K/V have scales of their own,
+ * k_soft_scale, v_soft_scale [Hkv][128 / block] (NULL where S == 0).  Set them per layer; all NULL clears them.  D = 64 or 128, Hq/Hkv <= 32,
+ * S <= 128.  No calibration is needed: whoever writes entries finds their scale.  With these dims
+ *   - confu_tree_attention computes the attention of the values the cache stands for, with bf16's precision: q and the softmax
+ *     weights are not rounded to 8 bits, nor is anything else but the output;
+ *   - confu_kv_append quantises bf16 rows and writes scales.  The smallest power of two 2^e, e >= -100, with amax <= 448 * 2^e (amax: the
+ *     largest finite magnitude of the call's rows in that block and head) is what the rows need; a block without prefix entries
+ *     gets that, any other the larger of that and its scale, and where it grows, the prefix entries of the block are encoded
+ *     again.  Entries are round to nearest even of value / scale, saturating at 448, NaN stays NaN.  So the pages that hold the slots from
+ *     the start of the prefix's last block must belong to the sequence alone;
+ *   - confu_kv_compact moves entries into blocks with other scales: a destination block's scale becomes the larger of
+ *     what it is and what the entries that move into it need (entries up to the root are encoded again where it grows), and the entries are
+ *     encoded with it.  It works on all layers at once and takes the arrays of all layers from
+ *     confu_set_kv_block_scale_layers: DEVICE arrays of n_layers device pointers (both NULL clears them).
+ */
+int confu_set_kv_block_scales(confu_ctx* ctx, float* k_scale, float* v_scale, const float* k_soft_scale,
+                              const float* v_soft_scale, int32_t block);
+int confu_set_kv_block_scale_layers(confu_ctx* ctx, float* const* k_scale_layers, float* const* v_scale_layers, int32_t block);
 
 const char* confu_status_string(int code);      /* host return codes and device status codes */
 const char* confu_last_cuda_error(const confu_ctx* ctx);
@@ -323,7 +349,8 @@ int confu_tree_accept_match(confu_ctx* ctx, int32_t B, int32_t T, int32_t C, int
  * For every layer l < n_layers and for K and V, in place:
  *   cache[seq_start[b] + P_b + k] = old cache[seq_start[b] + P_b + path[b][k]],  k = 1..accept_len[b]
  * (P_b = prefix_len[b]; slot P_b, the root, and the prefix stay), and
- * new_prefix_len[b] = P_b + accept_len[b] + 1.  Slots past the new prefix keep
+ * new_prefix_len[b] = P_b + accept_len[b] + 1 (a buffer of its own, not prefix_len: blocks of the kernel that start late still
+ * read that).  Slots past the new prefix keep
  * unspecified contents.  k_cache_layers / v_cache_layers: DEVICE arrays of
  * n_layers device pointers.  Uses dims->Hkv, D, kv_dtype, B, T.  All pointers device.
  * The path is checked on the device before anything moves: 0 <= accept_len[b] <=

@@ -17,7 +17,7 @@ MAX_TREE = 64
 MAX_ROWS = 128
 MAX_DEPTH = 63
 ACCEPT_LAZY = 0x100          # or-ed into sibling_mode: row statistics on demand
-BF16, F32, FP8_E4M3 = 0, 1, 2
+BF16, F32, FP8_E4M3, FP8_BLOCK = 0, 1, 2, 3
 OK = 0
 OPT_ATTENTION_PATH, OPT_WAIT_LIMIT_NS = 1, 2
 ATTENTION_AUTO, ATTENTION_GENERIC, ATTENTION_TENSOR, ATTENTION_TENSOR_PAIR, ATTENTION_TENSOR_NARROW = 0, 1, 2, 3, 4
@@ -29,7 +29,7 @@ EXPORTS = [
     "confu_accept_workspace_bytes", "confu_tree_accept", "confu_kv_compact", "confu_kv_append",
     "confu_tree_accept_static_max_rows", "confu_tree_accept_static", "confu_set_paging",
     "confu_tree_accept_match", "confu_con_embedding", "confu_set_option", "confu_attention_path",
-    "confu_selftest_bounded_wait", "confu_set_kv_scales",
+    "confu_selftest_bounded_wait", "confu_set_kv_scales", "confu_set_kv_block_scales", "confu_set_kv_block_scale_layers",
 ]
 
 
@@ -58,7 +58,7 @@ def lib():
         for n in ("confu_create", "confu_destroy", "confu_set_workspace", "confu_tree_plan", "confu_tree_attention",
                   "confu_tree_accept", "confu_kv_compact", "confu_kv_append", "confu_tree_accept_static", "confu_set_paging",
                   "confu_tree_accept_match", "confu_con_embedding", "confu_set_option", "confu_attention_path", "confu_selftest_bounded_wait",
-                  "confu_set_kv_scales"):
+                  "confu_set_kv_scales", "confu_set_kv_block_scales", "confu_set_kv_block_scale_layers"):
             getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -113,7 +113,8 @@ _DTYPES = {torch.bfloat16: BF16, torch.float32: F32, torch.uint8: FP8_E4M3, torc
 
 
 def dtype_code(dt):
-    return _DTYPES[dt]
+    """A torch dtype, or a type code itself (FP8_BLOCK has the torch dtype of FP8_E4M3)."""
+    return dt if isinstance(dt, int) else _DTYPES[dt]
 
 
 def make_dims(B, Hq, Hkv, D, T, Cn, S, dtype, sm_scale=0.0):
@@ -148,6 +149,17 @@ def confu_set_paging(ctx, block_table, max_pages=0):
 def confu_set_kv_scales(ctx, k_scale, v_scale):
     """k_scale, v_scale: fp32 CUDA tensors [Hkv] (kept alive by the caller), or None, None."""
     _check("confu_set_kv_scales", lib().confu_set_kv_scales(ctx, _ptr(k_scale), _ptr(v_scale)))
+
+
+def confu_set_kv_block_scales(ctx, k_scale, v_scale, k_soft_scale=None, v_soft_scale=None, block=0):
+    """fp32 CUDA tensors [pages, Hkv, 128 // block] and [Hkv, 128 // block] (kept alive by the caller), or None throughout."""
+    _done("confu_set_kv_block_scales", _native().set_kv_block_scales(ctx, k_scale, v_scale, k_soft_scale, v_soft_scale, block), ctx)
+
+
+def confu_set_kv_block_scale_layers(ctx, k_layer_ptrs, v_layer_ptrs, block=0):
+    """int64 CUDA tensors holding the per-layer addresses of the block scales (kept alive by the caller), or None, None."""
+    _check("confu_set_kv_block_scale_layers",
+           lib().confu_set_kv_block_scale_layers(ctx, _ptr(k_layer_ptrs), _ptr(v_layer_ptrs), C.c_int32(block)))
 
 
 def confu_set_option(ctx, option, value):

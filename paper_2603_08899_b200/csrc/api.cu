@@ -17,12 +17,16 @@ int check_dims(const confu_dims* d)
     if (d->B < 0 || d->Hq <= 0 || d->Hkv <= 0 || d->T <= 0 || d->C < 0 || d->S < 0) return CONFU_ERR_SHAPE;
     if (d->Hq % d->Hkv != 0) return CONFU_ERR_SHAPE;
     if (d->D != 64 && d->D != 128) return CONFU_ERR_SHAPE;
-    if (d->kv_dtype != CONFU_BF16 && d->kv_dtype != CONFU_F32 && d->kv_dtype != CONFU_FP8_E4M3) return CONFU_ERR_ARG;
+    if (d->kv_dtype < CONFU_BF16 || d->kv_dtype > CONFU_FP8_BLOCK) return CONFU_ERR_ARG;
     if (d->kv_dtype == CONFU_FP8_E4M3 && (d->D != 128 || d->Hq / d->Hkv > 4 || d->S > 128)) return CONFU_ERR_UNSUPPORTED;
+    if (d->kv_dtype == CONFU_FP8_BLOCK && (d->Hq / d->Hkv > kMaxTcGroup || d->S > 128)) return CONFU_ERR_UNSUPPORTED;
     if (d->T > CONFU_MAX_TREE || d->C > CONFU_MAX_TREE) return CONFU_ERR_UNSUPPORTED;
     if (!(d->sm_scale >= 0.f)) return CONFU_ERR_ARG;
     return CONFU_OK;
 }
+
+// tokens that share a scale in a block-scaled cache: a whole number of the 32 keys that a warp works on, within a page
+bool block_ok(int32_t block) { return block == 32 || block == 64 || block == 128; }
 
 int cuda_fail(confu_ctx* ctx, cudaError_t e)
 {
@@ -49,6 +53,15 @@ cudaError_t launch_attention_fp8(const Ctx* ctx, const confu_dims& d, const void
                                  const void* v_cache, int64_t n_slots, const SlotMap& map,
                                  const int32_t* prefix_len, const void* k_soft, const void* v_soft, const void* plan,
                                  void* partials, void* out, float* lse, int32_t* status, cudaStream_t st);
+cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache,
+                                   const void* v_cache, int64_t n_slots, const SlotMap& map, const int32_t* prefix_len,
+                                   const void* k_soft, const void* v_soft, const void* plan, void* partials, void* out,
+                                   float* lse, int32_t* status, cudaStream_t st);
+cudaError_t launch_append_block(const Ctx* ctx, const confu_dims& d, const void* k_rows, const void* v_rows, void* k_cache,
+                                void* v_cache, const SlotMap& map, const int32_t* prefix_len, cudaStream_t st);
+cudaError_t launch_compact_block(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers,
+                                 const SlotMap& map, const int32_t* prefix_len, const int32_t* accept_len, const int32_t* path,
+                                 int32_t* new_prefix_len, int32_t* status, cudaStream_t st);
 cudaError_t launch_append_fp8(int B, int R, int Hkv, int D, const void* k_rows, const void* v_rows, void* k_cache,
                               void* v_cache, const SlotMap& map, const int32_t* prefix_len, const float* k_scale,
                               const float* v_scale, cudaStream_t st);
@@ -80,6 +93,10 @@ int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
         const bool ok = ctx->attention_path == CONFU_ATTENTION_AUTO || ctx->attention_path == CONFU_ATTENTION_TENSOR;
         return ok && fp8_attention_supported(d) && ctx->sm_count >= n_rg ? (int)CONFU_ATTENTION_TENSOR : (int)CONFU_ERR_UNSUPPORTED;
     }
+    if (d.kv_dtype == CONFU_FP8_BLOCK) {
+        const bool ok = ctx->attention_path == CONFU_ATTENTION_AUTO || ctx->attention_path == CONFU_ATTENTION_GENERIC;
+        return ok && ctx->sm_count >= n_rg ? (int)CONFU_ATTENTION_GENERIC : (int)CONFU_ERR_UNSUPPORTED;
+    }
     switch (ctx->attention_path) {
         case CONFU_ATTENTION_GENERIC: return CONFU_ATTENTION_GENERIC;
         case CONFU_ATTENTION_TENSOR: return tc ? (int)CONFU_ATTENTION_TENSOR : (int)CONFU_ERR_UNSUPPORTED;
@@ -98,6 +115,7 @@ int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
 // row group: there have to be that many.  A path that the caller has chosen is taken as it is named.
 int plan_kind(const confu_ctx* ctx, const confu_dims& d, int path)
 {
+    if (d.kv_dtype == CONFU_FP8_BLOCK) return kPlanCta;
     if (path == CONFU_ATTENTION_TENSOR_PAIR) return kPlanPair;
     if (path == CONFU_ATTENTION_GENERIC && !tc_attention_supported(d) && !pair_attention_supported(d)) return kPlanMasks;
     const int n_tiles = row_groups(d.T + d.C, d.Hq / d.Hkv, 1);
@@ -122,6 +140,10 @@ int confu_create(confu_ctx** out, int device)
     c->max_pages = 0;
     c->last_error = cudaSuccess;
     c->k_scale = c->v_scale = nullptr;
+    c->k_block_scale = c->v_block_scale = nullptr;
+    c->k_soft_scale = c->v_soft_scale = nullptr;
+    c->k_block_layers = c->v_block_layers = nullptr;
+    c->block = c->layer_block = 0;
     c->attention_path = CONFU_ATTENTION_AUTO;
     c->wait_ns = 2000000000ull;
     cudaError_t e = cudaSetDevice(device);
@@ -171,6 +193,32 @@ int confu_set_kv_scales(confu_ctx* ctx, const float* k_scale, const float* v_sca
     if ((k_scale == nullptr) != (v_scale == nullptr)) return CONFU_ERR_ARG;
     ctx->k_scale = k_scale;
     ctx->v_scale = v_scale;
+    return CONFU_OK;
+}
+
+int confu_set_kv_block_scales(confu_ctx* ctx, float* k_scale, float* v_scale, const float* k_soft_scale,
+                              const float* v_soft_scale, int32_t block)
+{
+    if (!ctx) return CONFU_ERR_ARG;
+    if ((k_scale == nullptr) != (v_scale == nullptr) || (k_soft_scale == nullptr) != (v_soft_scale == nullptr)) return CONFU_ERR_ARG;
+    if (k_soft_scale && !k_scale) return CONFU_ERR_ARG;
+    if (k_scale && !block_ok(block)) return CONFU_ERR_ARG;
+    ctx->k_block_scale = k_scale;
+    ctx->v_block_scale = v_scale;
+    ctx->k_soft_scale = k_soft_scale;
+    ctx->v_soft_scale = v_soft_scale;
+    ctx->block = k_scale ? block : 0;
+    return CONFU_OK;
+}
+
+int confu_set_kv_block_scale_layers(confu_ctx* ctx, float* const* k_scale_layers, float* const* v_scale_layers, int32_t block)
+{
+    if (!ctx) return CONFU_ERR_ARG;
+    if ((k_scale_layers == nullptr) != (v_scale_layers == nullptr)) return CONFU_ERR_ARG;
+    if (k_scale_layers && !block_ok(block)) return CONFU_ERR_ARG;
+    ctx->k_block_layers = k_scale_layers;
+    ctx->v_block_layers = v_scale_layers;
+    ctx->layer_block = k_scale_layers ? block : 0;
     return CONFU_OK;
 }
 
@@ -280,6 +328,8 @@ int confu_tree_attention(confu_ctx* ctx, const confu_dims* dims, const void* q, 
     const int path = resolve_attention_path(ctx, *dims);
     if (path < 0) return path;
     if (dims->kv_dtype == CONFU_FP8_E4M3 && !ctx->k_scale) return CONFU_ERR_UNSUPPORTED;      // an E4M3 cache means nothing without its scales
+    if (dims->kv_dtype == CONFU_FP8_BLOCK &&
+        (!ctx->block_table || !ctx->k_block_scale || (dims->S > 0 && !ctx->k_soft_scale))) return CONFU_ERR_UNSUPPORTED;
     cudaStream_t st = (cudaStream_t)stream;
     char* ws = (char*)ctx->workspace;
     const void* use_plan = plan;
@@ -291,7 +341,10 @@ int confu_tree_attention(confu_ctx* ctx, const confu_dims* dims, const void* q, 
         use_plan = own_plan;
     }
     cudaError_t e;
-    if (path == CONFU_ATTENTION_TENSOR_PAIR)
+    if (dims->kv_dtype == CONFU_FP8_BLOCK)
+        e = launch_attention_block(ctx, *dims, q, k_cache, v_cache, n_slots, map, prefix_len, k_soft, v_soft, use_plan,
+                                   ws + ws_partial_offset(dims), out, lse, status, st);
+    else if (path == CONFU_ATTENTION_TENSOR_PAIR)
         e = launch_attention_pair(ctx, *dims, q, k_cache, v_cache, n_slots, map, prefix_len, k_soft, v_soft,
                                   use_plan, ws + ws_partial_offset(dims), out, lse, status, st);
     else if (path == CONFU_ATTENTION_TENSOR && dims->kv_dtype == CONFU_FP8_E4M3)
@@ -377,6 +430,12 @@ int confu_kv_compact(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, v
     if (!ctx->block_table && !seq_start) return CONFU_ERR_ARG;
     const SlotMap map = {seq_start, ctx->block_table, ctx->max_pages};
     if (n_layers > 0 && (!k_cache_layers || !v_cache_layers)) return CONFU_ERR_ARG;
+    if (dims->kv_dtype == CONFU_FP8_BLOCK && n_layers > 0) {
+        if (!ctx->block_table || !ctx->k_block_layers) return CONFU_ERR_UNSUPPORTED;
+        cudaError_t eb = launch_compact_block(ctx, *dims, n_layers, k_cache_layers, v_cache_layers, map, prefix_len, accept_len, path,
+                                              new_prefix_len, status, (cudaStream_t)stream);
+        return eb == cudaSuccess ? CONFU_OK : cuda_fail(ctx, eb);
+    }
     const int64_t row_bytes = (int64_t)dims->Hkv * dims->D * (dims->kv_dtype == CONFU_BF16 ? 2 : dims->kv_dtype == CONFU_F32 ? 4 : 1);
     cudaError_t e = launch_compact(ctx, dims->B, dims->T, n_layers, row_bytes, k_cache_layers, v_cache_layers, map,
                                    prefix_len, accept_len, path, new_prefix_len, status, (cudaStream_t)stream);
@@ -395,6 +454,11 @@ int confu_kv_append(confu_ctx* ctx, const confu_dims* dims, const void* k_rows, 
     const SlotMap map = {seq_start, ctx->block_table, ctx->max_pages};
     if (misaligned(k_rows) || misaligned(v_rows) || misaligned(k_cache) || misaligned(v_cache)) return CONFU_ERR_ALIGN;
     const int64_t row_bytes = (int64_t)dims->Hkv * dims->D * (dims->kv_dtype == CONFU_BF16 ? 2 : dims->kv_dtype == CONFU_F32 ? 4 : 1);
+    if (dims->kv_dtype == CONFU_FP8_BLOCK) {
+        if (!ctx->block_table || !ctx->k_block_scale) return CONFU_ERR_UNSUPPORTED;
+        cudaError_t eb = launch_append_block(ctx, *dims, k_rows, v_rows, k_cache, v_cache, map, prefix_len, (cudaStream_t)stream);
+        return eb == cudaSuccess ? CONFU_OK : cuda_fail(ctx, eb);
+    }
     if (dims->kv_dtype == CONFU_FP8_E4M3) {
         if (!ctx->k_scale) return CONFU_ERR_UNSUPPORTED;
         cudaError_t e8 = launch_append_fp8(dims->B, dims->T + dims->C, dims->Hkv, dims->D, k_rows, v_rows, k_cache, v_cache,

@@ -172,6 +172,12 @@ struct Ctx {
     const float* v_scale;
     int attention_path;            // CONFU_ATTENTION_* (confu_set_option)
     unsigned long long wait_ns;    // limit of the bounded waits inside the kernels
+    float *k_block_scale, *v_block_scale;              // block scales of a layer (confu_set_kv_block_scales)
+    const float *k_soft_scale, *v_soft_scale;
+    int block;                     // tokens per scale
+    float* const* k_block_layers;  // of all layers (confu_set_kv_block_scale_layers)
+    float* const* v_block_layers;
+    int layer_block;
 };
 
 // A function attribute (the opt-in to more than 48 KB of dynamic shared memory) belongs to a

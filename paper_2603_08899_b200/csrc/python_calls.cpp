@@ -225,6 +225,16 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args)
     END(confu_kv_append(ctx, dims, k_rows, v_rows, k, v, seq_start, prefix_len, st))
 }
 
+// (host state only, but called before every layer's calls)
+PyObject* set_kv_block_scales(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    BEGIN
+    confu_ctx* ctx = r.ctx();
+    auto k = r.as<float>(), v = r.as<float>(), ks = r.as<float>(), vs = r.as<float>();
+    const int block = (int)r.integer();
+    END(confu_set_kv_block_scales(ctx, k, v, ks, vs, block))
+}
+
 // hidden, experts give the sizes; the type code is the caller's
 PyObject* con_embedding(PyObject*, PyObject* const* args, Py_ssize_t n_args)
 {
@@ -250,7 +260,7 @@ PyObject* con_embedding(PyObject*, PyObject* const* args, Py_ssize_t n_args)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(tree_plan), FAST(tree_attention), FAST(tree_accept), FAST(tree_accept_match), FAST(kv_compact),
-                         FAST(kv_append), FAST(con_embedding), {nullptr, nullptr, 0, nullptr}};
+                         FAST(kv_append), FAST(set_kv_block_scales), FAST(con_embedding), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
