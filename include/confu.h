@@ -74,7 +74,9 @@ enum {
     CONFU_ST_DEGENERATE = 7,     /* residual distribution had no mass; target row used instead */
     CONFU_ST_TOO_DEEP = 8,       /* accepted path longer than CONFU_MAX_DEPTH */
     CONFU_ST_BAD_PATH = 9,       /* confu_kv_compact: path is not 0 = path[0] < path[1] < ... < T, or accept_len out of range */
-    CONFU_ST_BAD_PLAN = 10       /* confu_tree_attention: the plan was built for another attention path */
+    CONFU_ST_BAD_PLAN = 10,      /* confu_tree_attention: the plan was built for another attention path */
+    CONFU_ST_NO_PAGES = 11,      /* confu_pages_*: too few free pages; nothing was done for this request */
+    CONFU_ST_BAD_PAGES = 12      /* confu_pages_*: a row, a length or a page that there is not; nothing was done for this request */
 };
 
 enum { CONFU_BF16 = 0, CONFU_F32 = 1, CONFU_FP8_E4M3 = 2,    /* FP8: cache entries only, see confu_set_kv_scales */
@@ -375,6 +377,63 @@ int confu_kv_compact(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers,
 int confu_kv_append(confu_ctx* ctx, const confu_dims* dims, const void* k_rows, const void* v_rows,
                     void* k_cache, void* v_cache, const int64_t* seq_start, const int32_t* prefix_len,
                     void* stream);
+
+/* ---- pages of a paged pool ----------------------------------------------- */
+
+/*
+ * Who has which page of the paged pools (confu_set_paging; the paper has no cache layout).  All layers' pools have the same pages,
+ * so one table serves them.  ref_count[p] is the number of entries of the table that name page p (0: free); entries of a row are its pages
+ * in order, -1 (or any negative number) where it has none.  A program starts with counts of 0 and entries of -1 and lets these calls change
+ * them; block_table is what confu_set_paging is given.  Everything is on the device: no call reads anything back.
+ *
+ * A call works on n <= CONFU_MAX_PAGE_REQUESTS requests (CONFU_ERR_UNSUPPORTED beyond), device arrays of n int32 each; status: optional device int32
+ * [n], where a request that is not served leaves its code (the others are; nothing else is ever written there).  Free pages are
+ * handed out lowest first, in the order of the requests; when they run out, no later request of the call gets any.
+ */
+typedef struct {
+    int32_t n_pages;             /* pages of a pool: its slots / 128 */
+    int32_t n_rows, max_pages;   /* of the block table */
+    int32_t* ref_count;          /* device [n_pages] */
+    int32_t* block_table;        /* device [n_rows][max_pages] */
+} confu_pages;
+
+#define CONFU_MAX_PAGE_REQUESTS 1024
+
+/* Device scratch of confu_pages_fork and confu_pages_compact. */
+size_t confu_pages_workspace_bytes(int32_t n_pages);
+
+/* Row rows[i] gets the pages that it lacks for lengths[i] slots: ceil(lengths[i] / 128) entries (a step's rows count: prefix + R).  A row named
+ * twice is refused (CONFU_ST_BAD_PAGES) the second time. */
+int confu_pages_reserve(confu_ctx* ctx, const confu_pages* pages, int32_t n, const int32_t* rows, const int32_t* lengths,
+                        int32_t* status, void* stream);
+
+/*
+ * Row dst_rows[i], which has no pages, becomes a copy of the first lengths[i] slots of row src_rows[i]: whole pages are shared, the
+ * part-filled last one, which both will write to, is copied in all layers (K, V and, with kv_dtype CONFU_FP8_BLOCK, the block scales that
+ * confu_set_kv_block_scale_layers names) into a free page.  Refused (CONFU_ST_BAD_PAGES): a destination that has pages, is named twice or is a
+ * source of the same call, a source without the pages.  A source may be named often.  k_cache_layers, v_cache_layers: as for
+ * confu_kv_compact; uses dims->Hkv, D, kv_dtype.  A page that several rows name is not written by append or compaction as long as
+ * every row's prefix covers it whole, which this keeps.
+ */
+int confu_pages_fork(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, void* const* k_cache_layers, void* const* v_cache_layers,
+                     const confu_pages* pages, int32_t n, const int32_t* src_rows, const int32_t* dst_rows, const int32_t* lengths,
+                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* The rows lose all their pages; a page that no entry names any more is free.  A row may be named twice. */
+int confu_pages_free(confu_ctx* ctx, const confu_pages* pages, int32_t n, const int32_t* rows, int32_t* status, void* stream);
+
+/* Page src_pages[i] is copied to dst_pages[i] in all layers (with block scales, as above); neither table nor counts change.  No page may be
+ * both a source and a destination, or a destination twice; page ids outside the pool are skipped (CONFU_ST_BAD_PAGES).  Any n. */
+int confu_pages_copy(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, void* const* k_cache_layers, void* const* v_cache_layers,
+                     int32_t n_pages, int32_t n, const int32_t* src_pages, const int32_t* dst_pages, int32_t* status, void* stream);
+
+/*
+ * The pages in use (ref_count > 0) become the first ones of the pools: with u of them, those that lie at u or behind, in order, move to
+ * the free places before u, in order, in all layers; table and counts follow.  n_used (device int32): u.  page_map (device int32
+ * [n_pages], may be NULL): the new id of every page, -1 for a free one, for ids that a program keeps elsewhere.
+ */
+int confu_pages_compact(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, void* const* k_cache_layers, void* const* v_cache_layers,
+                        const confu_pages* pages, int32_t* page_map, int32_t* n_used, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- contemplate-token embedding (Sec. 3.2, "Dynamic Contemplate Tokens with MoE") ---- */
 

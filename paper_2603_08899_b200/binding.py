@@ -21,7 +21,8 @@ BF16, F32, FP8_E4M3, FP8_BLOCK = 0, 1, 2, 3
 OK = 0
 OPT_ATTENTION_PATH, OPT_WAIT_LIMIT_NS = 1, 2
 ATTENTION_AUTO, ATTENTION_GENERIC, ATTENTION_TENSOR, ATTENTION_TENSOR_PAIR, ATTENTION_TENSOR_NARROW = 0, 1, 2, 3, 4
-ST_TIMEOUT, ST_BAD_PATH, ST_BAD_PLAN = 6, 9, 10
+ST_TIMEOUT, ST_BAD_PATH, ST_BAD_PLAN, ST_NO_PAGES, ST_BAD_PAGES = 6, 9, 10, 11, 12
+MAX_PAGE_REQUESTS = 1024
 
 EXPORTS = [
     "confu_create", "confu_destroy", "confu_workspace_bytes", "confu_set_workspace", "confu_status_string",
@@ -30,12 +31,17 @@ EXPORTS = [
     "confu_tree_accept_static_max_rows", "confu_tree_accept_static", "confu_set_paging",
     "confu_tree_accept_match", "confu_con_embedding", "confu_set_option", "confu_attention_path",
     "confu_selftest_bounded_wait", "confu_set_kv_scales", "confu_set_kv_block_scales", "confu_set_kv_block_scale_layers",
+    "confu_pages_workspace_bytes", "confu_pages_reserve", "confu_pages_fork", "confu_pages_free", "confu_pages_copy", "confu_pages_compact",
 ]
 
 
 class ConfuDims(C.Structure):
     _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("T", C.c_int32),
                 ("C", C.c_int32), ("S", C.c_int32), ("kv_dtype", C.c_int32), ("sm_scale", C.c_float)]
+
+
+class ConfuPages(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("n_rows", C.c_int32), ("max_pages", C.c_int32), ("ref_count", C.c_void_p), ("block_table", C.c_void_p)]
 
 
 _lib = None
@@ -53,6 +59,7 @@ def lib():
         L.confu_plan_bytes.restype = C.c_size_t
         L.confu_accept_workspace_bytes.restype = C.c_size_t
         L.confu_tree_accept_static_max_rows.restype = C.c_size_t
+        L.confu_pages_workspace_bytes.restype = C.c_size_t
         L.confu_status_string.restype = C.c_char_p
         L.confu_last_cuda_error.restype = C.c_char_p
         for n in ("confu_create", "confu_destroy", "confu_set_workspace", "confu_tree_plan", "confu_tree_attention",
@@ -119,6 +126,12 @@ def dtype_code(dt):
 
 def make_dims(B, Hq, Hkv, D, T, Cn, S, dtype, sm_scale=0.0):
     return ConfuDims(B, Hq, Hkv, D, T, Cn, S, dtype_code(dtype), float(sm_scale))
+
+
+def make_pages(ref_count, block_table):
+    """ref_count: int32 CUDA tensor [n_pages], block_table: int32 CUDA tensor [n_rows, max_pages] (kept alive by the caller)."""
+    assert ref_count.dtype == torch.int32 and block_table.dtype == torch.int32 and block_table.dim() == 2
+    return ConfuPages(ref_count.numel(), block_table.shape[0], block_table.shape[1], _ptr(ref_count), _ptr(block_table))
 
 
 # --------------------------------------------------------------------------- entry points
@@ -252,3 +265,33 @@ def confu_kv_compact(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, seq_start,
 def confu_kv_append(ctx, dims, k_rows, v_rows, k_cache, v_cache, seq_start, prefix_len, stream=None):
     _done("confu_kv_append",
           _native().kv_append(ctx, dims, k_rows, v_rows, k_cache, v_cache, seq_start, prefix_len, stream), ctx)
+
+
+def confu_pages_workspace_bytes(n_pages):
+    return int(lib().confu_pages_workspace_bytes(C.c_int32(n_pages)))
+
+
+def confu_pages_reserve(ctx, pages, rows, lengths, status=None, stream=None):
+    """rows, lengths (and status): int32 CUDA tensors of a request each."""
+    _done("confu_pages_reserve", _native().pages_reserve(ctx, pages, rows, lengths, status, stream), ctx)
+
+
+def confu_pages_fork(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, pages, src_rows, dst_rows, lengths, workspace, status=None, stream=None):
+    """k_layer_ptrs / v_layer_ptrs: int64 CUDA tensors holding the per-layer pool addresses."""
+    _done("confu_pages_fork",
+          _native().pages_fork(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, pages, src_rows, dst_rows, lengths, workspace, status, stream), ctx)
+
+
+def confu_pages_free(ctx, pages, rows, status=None, stream=None):
+    _done("confu_pages_free", _native().pages_free(ctx, pages, rows, status, stream), ctx)
+
+
+def confu_pages_copy(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, n_pages, src_pages, dst_pages, status=None, stream=None):
+    _done("confu_pages_copy",
+          _native().pages_copy(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, n_pages, src_pages, dst_pages, status, stream), ctx)
+
+
+def confu_pages_compact(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, pages, page_map, n_used, workspace, stream=None):
+    """page_map: int32 CUDA tensor [n_pages] or None; n_used: int32 CUDA tensor [1]."""
+    _done("confu_pages_compact",
+          _native().pages_compact(ctx, dims, n_layers, k_layer_ptrs, v_layer_ptrs, pages, page_map, n_used, workspace, stream), ctx)

@@ -28,6 +28,23 @@ int check_dims(const confu_dims* d)
 // tokens that share a scale in a block-scaled cache: a whole number of the 32 keys that a warp works on, within a page
 bool block_ok(int32_t block) { return block == 32 || block == 64 || block == 128; }
 
+int check_pages(const confu_pages* p, int32_t n)
+{
+    if (!p || n < 0 || !p->ref_count || !p->block_table) return CONFU_ERR_ARG;
+    if (p->n_pages <= 0 || p->n_rows <= 0 || p->max_pages <= 0) return CONFU_ERR_SHAPE;
+    if (n > CONFU_MAX_PAGE_REQUESTS) return CONFU_ERR_UNSUPPORTED;
+    return misaligned(p->ref_count) || misaligned(p->block_table) ? CONFU_ERR_ALIGN : CONFU_OK;
+}
+
+// what a page is made of: Hkv, D and kv_dtype of the dims, and the layers' pools
+int check_page_pools(const confu_ctx* ctx, const confu_dims* d, int32_t n_layers, void* const* k, void* const* v)
+{
+    const int rc = check_dims(d);
+    if (rc != CONFU_OK) return rc;
+    if (n_layers < 0 || (n_layers > 0 && (!k || !v))) return CONFU_ERR_ARG;
+    return n_layers > 0 && d->kv_dtype == CONFU_FP8_BLOCK && !ctx->k_block_layers ? CONFU_ERR_UNSUPPORTED : CONFU_OK;
+}
+
 int cuda_fail(confu_ctx* ctx, cudaError_t e)
 {
     if (ctx) ctx->last_error = e;
@@ -53,6 +70,15 @@ cudaError_t launch_attention_fp8(const Ctx* ctx, const confu_dims& d, const void
                                  const void* v_cache, int64_t n_slots, const SlotMap& map,
                                  const int32_t* prefix_len, const void* k_soft, const void* v_soft, const void* plan,
                                  void* partials, void* out, float* lse, int32_t* status, cudaStream_t st);
+size_t pages_workspace_bytes(int n_pages);
+cudaError_t launch_pages_reserve(const confu_pages& pg, int n, const int32_t* rows, const int32_t* lengths, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_fork(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, const confu_pages& pg, int n,
+                              const int32_t* src_rows, const int32_t* dst_rows, const int32_t* lengths, void* workspace, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_free(const confu_pages& pg, int n, const int32_t* rows, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_compact(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, const confu_pages& pg,
+                                 int32_t* page_map, int32_t* n_used, void* workspace, cudaStream_t st);
+cudaError_t launch_pages_copy(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, int n_pages, int n,
+                              const int32_t* src_pages, const int32_t* dst_pages, int32_t* status, cudaStream_t st);
 cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache,
                                    const void* v_cache, int64_t n_slots, const SlotMap& map, const int32_t* prefix_len,
                                    const void* k_soft, const void* v_soft, const void* plan, void* partials, void* out,
@@ -274,6 +300,8 @@ const char* confu_status_string(int code)
         case CONFU_ST_DEGENERATE: return "residual distribution without mass";
         case CONFU_ST_TOO_DEEP: return "accepted path longer than CONFU_MAX_DEPTH";
         case CONFU_ST_BAD_PATH: return "accepted path is not an increasing chain of tree nodes from the root";
+        case CONFU_ST_NO_PAGES: return "too few free pages";
+        case CONFU_ST_BAD_PAGES: return "row, length or page out of range, or a row that does not fit the request";
         case CONFU_ST_BAD_PLAN: return "plan was built for another attention path";
         default: return "unknown code";
     }
@@ -467,6 +495,70 @@ int confu_kv_append(confu_ctx* ctx, const confu_dims* dims, const void* k_rows, 
     }
     cudaError_t e = launch_append(dims->B, dims->T + dims->C, row_bytes, k_rows, v_rows, k_cache, v_cache, map,
                                   prefix_len, (cudaStream_t)stream);
+    return e == cudaSuccess ? CONFU_OK : cuda_fail(ctx, e);
+}
+
+size_t confu_pages_workspace_bytes(int32_t n_pages) { return n_pages > 0 ? pages_workspace_bytes(n_pages) : 0; }
+
+int confu_pages_reserve(confu_ctx* ctx, const confu_pages* pages, int32_t n, const int32_t* rows, const int32_t* lengths,
+                        int32_t* status, void* stream)
+{
+    if (!ctx) return CONFU_ERR_ARG;
+    const int rc = check_pages(pages, n);
+    if (rc != CONFU_OK || n == 0) return rc;
+    if (!rows || !lengths) return CONFU_ERR_ARG;
+    const cudaError_t e = launch_pages_reserve(*pages, n, rows, lengths, status, (cudaStream_t)stream);
+    return e == cudaSuccess ? CONFU_OK : cuda_fail(ctx, e);
+}
+
+int confu_pages_fork(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, void* const* k_cache_layers, void* const* v_cache_layers,
+                     const confu_pages* pages, int32_t n, const int32_t* src_rows, const int32_t* dst_rows, const int32_t* lengths,
+                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream)
+{
+    if (!ctx) return CONFU_ERR_ARG;
+    int rc = check_pages(pages, n);
+    if (rc == CONFU_OK) rc = check_page_pools(ctx, dims, n_layers, k_cache_layers, v_cache_layers);
+    if (rc != CONFU_OK || n == 0) return rc;
+    if (!src_rows || !dst_rows || !lengths) return CONFU_ERR_ARG;
+    if (misaligned(workspace)) return CONFU_ERR_ALIGN;
+    if (!workspace || workspace_bytes < pages_workspace_bytes(pages->n_pages)) return CONFU_ERR_WORKSPACE;
+    const cudaError_t e = launch_pages_fork(ctx, *dims, n_layers, k_cache_layers, v_cache_layers, *pages, n, src_rows, dst_rows, lengths, workspace, status,
+                                            (cudaStream_t)stream);
+    return e == cudaSuccess ? CONFU_OK : cuda_fail(ctx, e);
+}
+
+int confu_pages_free(confu_ctx* ctx, const confu_pages* pages, int32_t n, const int32_t* rows, int32_t* status, void* stream)
+{
+    if (!ctx) return CONFU_ERR_ARG;
+    const int rc = check_pages(pages, n);
+    if (rc != CONFU_OK || n == 0) return rc;
+    if (!rows) return CONFU_ERR_ARG;
+    const cudaError_t e = launch_pages_free(*pages, n, rows, status, (cudaStream_t)stream);
+    return e == cudaSuccess ? CONFU_OK : cuda_fail(ctx, e);
+}
+
+int confu_pages_copy(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, void* const* k_cache_layers, void* const* v_cache_layers,
+                     int32_t n_pages, int32_t n, const int32_t* src_pages, const int32_t* dst_pages, int32_t* status, void* stream)
+{
+    if (!ctx || n < 0 || n_pages <= 0) return CONFU_ERR_ARG;
+    const int rc = check_page_pools(ctx, dims, n_layers, k_cache_layers, v_cache_layers);
+    if (rc != CONFU_OK || n == 0) return rc;
+    if (!src_pages || !dst_pages) return CONFU_ERR_ARG;
+    const cudaError_t e = launch_pages_copy(ctx, *dims, n_layers, k_cache_layers, v_cache_layers, n_pages, n, src_pages, dst_pages, status, (cudaStream_t)stream);
+    return e == cudaSuccess ? CONFU_OK : cuda_fail(ctx, e);
+}
+
+int confu_pages_compact(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, void* const* k_cache_layers, void* const* v_cache_layers,
+                        const confu_pages* pages, int32_t* page_map, int32_t* n_used, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return CONFU_ERR_ARG;
+    int rc = check_pages(pages, 0);
+    if (rc == CONFU_OK) rc = check_page_pools(ctx, dims, n_layers, k_cache_layers, v_cache_layers);
+    if (rc != CONFU_OK) return rc;
+    if (!n_used) return CONFU_ERR_ARG;
+    if (misaligned(workspace)) return CONFU_ERR_ALIGN;
+    if (!workspace || workspace_bytes < pages_workspace_bytes(pages->n_pages)) return CONFU_ERR_WORKSPACE;
+    const cudaError_t e = launch_pages_compact(ctx, *dims, n_layers, k_cache_layers, v_cache_layers, *pages, page_map, n_used, workspace, (cudaStream_t)stream);
     return e == cudaSuccess ? CONFU_OK : cuda_fail(ctx, e);
 }
 

@@ -1,0 +1,447 @@
+// Pages of a paged pool: who has which, handed out, shared, taken back, copied, moved together.
+//
+// The state is two device arrays: the block table (a row of page ids per sequence, -1: none) and a count per page of the
+// entries that name it (0: free).  Requests name rows; a call works on all of them at once, and what it does is the same whatever order
+// blocks run in: free pages are handed out lowest first, in the order of the requests, entries of a request in order.
+//
+// Bookkeeping is one CTA (a chain of dependent reads and block-wide scans: latency), which leaves a list of pages to copy; a second kernel
+// copies them in all layers, K, V and block scales, and is bound by HBM: a page of 8 kv heads of 128 is 128 KB of E4M3 or 256 KB of bf16,
+// twice per layer.
+#include "common.cuh"
+
+namespace confu {
+
+namespace {
+
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+
+// Exclusive prefix sum over the CTA's threads; `total` for all of them.  `slots`: a word per warp.
+__device__ __forceinline__ int cta_scan(int v, int* slots, int& total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = v;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, incl, k);
+        if (lane >= k) incl += t;
+    }
+    __syncthreads();                                 // the last call's slots have been read
+    if (lane == 31) slots[warp] = incl;
+    __syncthreads();
+    int w = slots[lane], before = lane < warp ? w : 0;
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) {
+        w += __shfl_xor_sync(0xffffffffu, w, k);
+        before += __shfl_xor_sync(0xffffffffu, before, k);
+    }
+    total = w;
+    return before + incl - v;
+}
+
+// Four counts of pages p .. p + 3 (1: not there).
+__device__ __forceinline__ int4 four_counts(const int32_t* ref, int n_pages, int p)
+{
+    if (p + 3 < n_pages) return *reinterpret_cast<const int4*>(ref + p);
+    return make_int4(p < n_pages ? ref[p] : 1, p + 1 < n_pages ? ref[p + 1] : 1, p + 2 < n_pages ? ref[p + 2] : 1, 1);
+}
+
+// The first `want` free pages, lowest first, through put(rank, page); returns how many there are of them.
+template <typename Put> __device__ __forceinline__ int find_free(const int32_t* ref, int n_pages, int want, int* slots, Put put)
+{
+    int found = 0;
+    for (int base = 0; base < n_pages && found < want; base += 4 * kThreads) {
+        const int p = base + 4 * threadIdx.x;
+        const int4 c = four_counts(ref, n_pages, p);
+        const int cc[4] = {c.x, c.y, c.z, c.w};
+        int n = 0, total;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += p + i < n_pages && cc[i] == 0;
+        int at = found + cta_scan(n, slots, total);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (p + i < n_pages && cc[i] == 0) {
+                if (at < want) put(at, p + i);
+                ++at;
+            }
+        found += total;
+    }
+    return min(found, want);
+}
+
+// Whether row `row` is among those of the requests before i; `rows` in shared memory.
+__device__ __forceinline__ bool named_before(const int32_t* rows, int i)
+{
+    bool twice = false;
+    for (int j = 0; j < i; ++j) twice = twice || rows[j] == rows[i];
+    return twice;
+}
+
+// One CTA: the entries that a row lacks, counted, then filled.
+__global__ void __launch_bounds__(kThreads) pages_reserve_kernel(confu_pages pg, int n, const int32_t* __restrict__ rows,
+                                                                 const int32_t* __restrict__ lengths, int32_t* __restrict__ status)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ int32_t s_row[CONFU_MAX_PAGE_REQUESTS], s_need[CONFU_MAX_PAGE_REQUESTS], s_first[CONFU_MAX_PAGE_REQUESTS], s_lacks[CONFU_MAX_PAGE_REQUESTS];
+    __shared__ int slots[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int need = 0;
+    if (tid < n) {
+        const int len = lengths[tid];
+        s_row[tid] = rows[tid];
+        need = len < 0 ? -1 : (int)(((int64_t)len + kTileKeys - 1) / kTileKeys);
+    }
+    __syncthreads();
+    if (tid < n) {
+        const int row = s_row[tid];
+        if (row < 0 || row >= pg.n_rows || need < 0 || need > pg.max_pages || named_before(s_row, tid)) {
+            need = -1;
+            if (status) status[tid] = CONFU_ST_BAD_PAGES;
+        }
+        s_need[tid] = need;
+    }
+    __syncthreads();
+    for (int i = warp; i < n; i += kWarps) {         // entries that are not there yet
+        const int32_t* row = pg.block_table + (size_t)s_row[i] * pg.max_pages;
+        int lacks = 0;
+        for (int j = lane; j < s_need[i]; j += 32) lacks += row[j] < 0;
+        lacks = __reduce_add_sync(0xffffffffu, lacks);
+        if (lane == 0) s_lacks[i] = lacks;
+    }
+    __syncthreads();
+    int total;
+    const int lacks = tid < n ? s_lacks[tid] : 0;
+    const int first = cta_scan(lacks, slots, total);
+    if (tid < n) s_first[tid] = first;
+    // how many free pages there are, up to what is asked for
+    const int found = find_free(pg.ref_count, pg.n_pages, total, slots, [](int, int) {});
+    if (tid < n && lacks > 0 && first + lacks > found) {
+        s_need[tid] = -1;
+        if (status) status[tid] = CONFU_ST_NO_PAGES;
+    }
+    __syncthreads();
+    // requests are served in order, and from the first that there are too few pages for nothing more is handed out: page `rank` is for the
+    // entry with that rank, whose request is found by bisection
+    int served = tid < n && lacks > 0 && s_need[tid] >= 0 ? first + lacks : 0;
+    served = __reduce_max_sync(0xffffffffu, served);
+    __syncthreads();
+    if (lane == 0) slots[warp] = served;
+    __syncthreads();
+    served = __reduce_max_sync(0xffffffffu, slots[lane]);
+    __syncthreads();
+    find_free(pg.ref_count, pg.n_pages, served, slots, [&](int rank, int page) {
+        int lo = 0;
+        for (int hi = n; lo + 1 < hi;) {             // the last request whose first rank is not behind it
+            const int mid = (lo + hi) / 2;
+            if (s_first[mid] <= rank) lo = mid;
+            else hi = mid;
+        }
+        int32_t* row = pg.block_table + (size_t)s_row[lo] * pg.max_pages;
+        // entry number rank - first among the missing ones; they are filled by threads of one call of put at a time, but a missing
+        // entry stays recognisable: it is written as -2 - page and turned round below
+        int left = rank - s_first[lo];
+        for (int j = 0; j < s_need[lo]; ++j)
+            if (row[j] < 0 && left-- == 0) {
+                row[j] = -2 - page;
+                break;
+            }
+    });
+    __syncthreads();
+    for (int i = warp; i < n; i += kWarps) {
+        int32_t* row = pg.block_table + (size_t)s_row[i] * pg.max_pages;
+        for (int j = lane; j < s_need[i]; j += 32)
+            if (row[j] < -1) {
+                const int page = -2 - row[j];
+                row[j] = page;
+                pg.ref_count[page] = 1;
+            }
+    }
+}
+
+// Copies to make: count, then pairs.
+struct CopyList {
+    int32_t* count;
+    int2* pairs;
+};
+__host__ __device__ inline CopyList copy_list(void* workspace) { return {(int32_t*)workspace, (int2*)((char*)workspace + 256)}; }
+
+// One CTA: rows checked, a free page for every part-filled one, rows written, counts raised.
+__global__ void __launch_bounds__(kThreads) pages_fork_kernel(confu_pages pg, int n, const int32_t* __restrict__ src_rows,
+                                                              const int32_t* __restrict__ dst_rows, const int32_t* __restrict__ lengths,
+                                                              void* workspace, int32_t* __restrict__ status)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ int32_t s_src[CONFU_MAX_PAGE_REQUESTS], s_dst[CONFU_MAX_PAGE_REQUESTS], s_len[CONFU_MAX_PAGE_REQUESTS];
+    __shared__ int32_t s_page[CONFU_MAX_PAGE_REQUESTS];      // first: whether a request stands; then the page for its part-filled one
+    __shared__ int32_t s_free[CONFU_MAX_PAGE_REQUESTS];
+    __shared__ int slots[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid < n) {
+        s_src[tid] = src_rows[tid];
+        s_dst[tid] = dst_rows[tid];
+        s_len[tid] = lengths[tid];
+    }
+    __syncthreads();
+    if (tid < n) {
+        const int src = s_src[tid], dst = s_dst[tid], len = s_len[tid];
+        bool ok = src >= 0 && src < pg.n_rows && dst >= 0 && dst < pg.n_rows && len >= 0 && (int64_t)len <= (int64_t)pg.max_pages * kTileKeys;
+        ok = ok && !named_before(s_dst, tid);
+        for (int j = 0; ok && j < n; ++j) ok = s_src[j] != dst;      // (a row that is continued is not one that begins)
+        s_page[tid] = ok;
+    }
+    __syncthreads();
+    for (int i = warp; i < n; i += kWarps) {         // the source has the pages, the destination none
+        if (!s_page[i]) continue;
+        const int32_t *from = pg.block_table + (size_t)s_src[i] * pg.max_pages, *to = pg.block_table + (size_t)s_dst[i] * pg.max_pages;
+        const int need = (s_len[i] + kTileKeys - 1) / kTileKeys;
+        bool ok = true;
+        for (int j = lane; j < pg.max_pages; j += 32) {
+            if (j < need) ok = ok && from[j] >= 0 && from[j] < pg.n_pages;
+            ok = ok && to[j] < 0;
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        __syncwarp();
+        if (lane == 0) s_page[i] = ok;
+    }
+    __syncthreads();
+    const bool ok = tid < n && s_page[tid], part = ok && s_len[tid] % kTileKeys != 0;
+    int total;
+    const int rank = cta_scan(part, slots, total);
+    const int found = find_free(pg.ref_count, pg.n_pages, total, slots, [&](int at, int page) { s_free[at] = page; });
+    __syncthreads();
+    const CopyList copies = copy_list(workspace);
+    if (tid == 0) *copies.count = found;
+    if (tid < n) {
+        if (!ok || (part && rank >= found)) {
+            s_page[tid] = -2;                        // nothing is done
+            if (status) status[tid] = ok ? CONFU_ST_NO_PAGES : CONFU_ST_BAD_PAGES;
+        } else if (part) {
+            const int page = s_free[rank], from = pg.block_table[(size_t)s_src[tid] * pg.max_pages + s_len[tid] / kTileKeys];
+            s_page[tid] = page;
+            copies.pairs[rank] = make_int2(from, page);
+            pg.ref_count[page] = 1;
+        } else
+            s_page[tid] = -1;
+    }
+    __syncthreads();
+    for (int i = warp; i < n; i += kWarps) {
+        if (s_page[i] == -2) continue;
+        const int32_t* from = pg.block_table + (size_t)s_src[i] * pg.max_pages;
+        int32_t* to = pg.block_table + (size_t)s_dst[i] * pg.max_pages;
+        const int full = s_len[i] / kTileKeys;
+        for (int j = lane; j < full; j += 32) {
+            const int page = from[j];
+            to[j] = page;
+            atomicAdd(pg.ref_count + page, 1);
+        }
+        if (lane == 0 && s_page[i] >= 0) to[full] = s_page[i];
+    }
+}
+
+// A warp per row; an entry is taken out once, whoever names its row how often.
+__global__ void __launch_bounds__(256) pages_free_kernel(confu_pages pg, int n, const int32_t* __restrict__ rows, int32_t* __restrict__ status)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (i >= n) return;
+    const int row = rows[i];
+    if (row < 0 || row >= pg.n_rows) {
+        if (lane == 0 && status) status[i] = CONFU_ST_BAD_PAGES;
+        return;
+    }
+    int32_t* entry = pg.block_table + (size_t)row * pg.max_pages;
+    bool bad = false;
+    for (int j = lane; j < pg.max_pages; j += 32) {
+        if (entry[j] < 0) continue;
+        const int page = atomicExch(entry + j, -1);
+        if (page >= pg.n_pages) bad = true;
+        else if (page >= 0) atomicSub(pg.ref_count + page, 1);
+    }
+    if (__any_sync(0xffffffffu, bad) && lane == 0 && status) status[i] = CONFU_ST_BAD_PAGES;
+}
+
+// One CTA: pages in use counted (n_used); those behind the first n_used pages, in order, go to the free places among them, in order.
+__global__ void __launch_bounds__(kThreads) pages_map_kernel(confu_pages pg, int32_t* __restrict__ page_map, int32_t* __restrict__ n_used, void* workspace)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ int slots[kWarps];
+    const int tid = threadIdx.x;
+    const CopyList copies = copy_list(workspace);
+    int mine = 0, used;
+    for (int p = 4 * tid; p < pg.n_pages; p += 4 * kThreads) {
+        const int4 c = four_counts(pg.ref_count, pg.n_pages, p);
+        mine += (c.x > 0) + (p + 1 < pg.n_pages && c.y > 0) + (p + 2 < pg.n_pages && c.z > 0) + (p + 3 < pg.n_pages && c.w > 0);
+    }
+    cta_scan(mine, slots, used);
+    int holes = 0, movers = 0;
+    for (int base = 0; base < pg.n_pages; base += 4 * kThreads) {
+        const int p = base + 4 * tid;
+        const int4 c = four_counts(pg.ref_count, pg.n_pages, p);
+        const int cc[4] = {c.x, c.y, c.z, c.w};
+        int h = 0, m = 0, n_h, n_m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (p + i >= pg.n_pages) continue;
+            h += cc[i] <= 0 && p + i < used;
+            m += cc[i] > 0 && p + i >= used;
+        }
+        int at_h = holes + cta_scan(h, slots, n_h), at_m = movers + cta_scan(m, slots, n_m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (p + i >= pg.n_pages) continue;
+            page_map[p + i] = cc[i] > 0 ? p + i : -1;
+            if (cc[i] <= 0 && p + i < used) copies.pairs[at_h++].y = p + i;
+            if (cc[i] > 0 && p + i >= used) copies.pairs[at_m++].x = p + i;
+        }
+        holes += n_h;
+        movers += n_m;
+    }
+    __syncthreads();                                 // (as many holes as movers: the first n_used pages hold all the others)
+    for (int i = tid; i < movers; i += kThreads) {
+        const int2 c = copies.pairs[i];
+        page_map[c.x] = c.y;
+        pg.ref_count[c.y] = pg.ref_count[c.x];
+        pg.ref_count[c.x] = 0;
+    }
+    if (tid == 0) {
+        *copies.count = movers;
+        *n_used = used;
+    }
+}
+
+// What a page is in every layer.
+struct PagePools {
+    void* const* layers[2];                          // K, V
+    float* const* scales[2];                         // of block-scaled caches, else NULL
+    int n_layers, n_pages;
+    int vecs;                                        // 16-byte pieces of a page
+    int scale_floats;                                // block scales of a page
+};
+
+// Copies the list's pages in all layers, a piece of 16 KB at a time, and renumbers the block table where there is a map.
+constexpr int kCopyThreads = 256, kCopyPer = 4, kPiece = kCopyThreads * kCopyPer;
+__global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const PagePools pools, const int32_t* __restrict__ count, int n_given,
+                                                                  const int2* __restrict__ pairs, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                                  int32_t* __restrict__ status, confu_pages pg, const int32_t* __restrict__ page_map)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (page_map)
+        for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < (int64_t)pg.n_rows * pg.max_pages; i += (int64_t)gridDim.x * kCopyThreads) {
+            const int page = pg.block_table[i];
+            if (page >= 0 && page < pg.n_pages) pg.block_table[i] = page_map[page];
+        }
+    const int n = count ? *count : n_given;
+    const int per_page = (pools.vecs + kPiece - 1) / kPiece;
+    const int64_t items = (int64_t)n * 2 * pools.n_layers * per_page;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int piece = (int)(it % per_page);
+        const int64_t rest = it / per_page;
+        const int kv = (int)(rest & 1), layer = (int)((rest >> 1) % pools.n_layers), i = (int)((rest >> 1) / pools.n_layers);
+        const int2 c = pairs ? pairs[i] : make_int2(src[i], dst[i]);
+        if ((uint32_t)c.x >= (uint32_t)pools.n_pages || (uint32_t)c.y >= (uint32_t)pools.n_pages) {
+            if (status && threadIdx.x == 0) status[i] = CONFU_ST_BAD_PAGES;
+            continue;
+        }
+        if (c.x == c.y) continue;
+        uint4* pool = static_cast<uint4*>(pools.layers[kv][layer]);
+        const uint4* from = pool + (size_t)c.x * pools.vecs;
+        uint4* to = pool + (size_t)c.y * pools.vecs;
+        uint4 v[kCopyPer];
+#pragma unroll
+        for (int k = 0; k < kCopyPer; ++k) {
+            const int at = piece * kPiece + k * kCopyThreads + threadIdx.x;
+            if (at < pools.vecs) v[k] = __ldcs(from + at);
+        }
+#pragma unroll
+        for (int k = 0; k < kCopyPer; ++k) {
+            const int at = piece * kPiece + k * kCopyThreads + threadIdx.x;
+            if (at < pools.vecs) __stcs(to + at, v[k]);
+        }
+        if (pools.scale_floats && piece == 0) {
+            float* scales = pools.scales[kv][layer];
+            for (int k = threadIdx.x; k < pools.scale_floats; k += kCopyThreads)
+                scales[(size_t)c.y * pools.scale_floats + k] = scales[(size_t)c.x * pools.scale_floats + k];
+        }
+    }
+}
+
+PagePools pools_of(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, int n_pages)
+{
+    PagePools p = {};
+    p.layers[0] = k_layers;
+    p.layers[1] = v_layers;
+    p.n_layers = n_layers;
+    p.n_pages = n_pages;
+    p.vecs = kTileKeys * d.Hkv * d.D * (d.kv_dtype == CONFU_BF16 ? 2 : d.kv_dtype == CONFU_F32 ? 4 : 1) / 16;
+    if (d.kv_dtype == CONFU_FP8_BLOCK) {
+        p.scales[0] = ctx->k_block_layers;
+        p.scales[1] = ctx->v_block_layers;
+        p.scale_floats = n_layers ? d.Hkv * (kTileKeys / ctx->layer_block) : 0;
+    }
+    return p;
+}
+
+cudaError_t copy(const Ctx* ctx, const PagePools& p, int64_t most, const int32_t* count, const int2* pairs, const int32_t* src, const int32_t* dst, int32_t* status,
+                 const confu_pages& pg, const int32_t* page_map, cudaStream_t st)
+{
+    const int64_t items = most * 2 * p.n_layers * ((p.vecs + kPiece - 1) / kPiece), resident = (int64_t)ctx->sm_count * 8;
+    const int64_t table = page_map ? ((int64_t)pg.n_rows * pg.max_pages + kCopyThreads - 1) / kCopyThreads : 0;
+    const int64_t blocks = items > table ? items : table;
+    if (blocks == 0) return cudaSuccess;
+    return launch_pdl(pages_copy_kernel, dim3((unsigned)(blocks < resident ? blocks : resident)), dim3(kCopyThreads), st, p, count, (int)most, pairs, src, dst,
+                      status, pg, page_map);
+}
+
+}  // namespace
+
+// count and up to one pair per page or request; then a map where the caller has no use for one
+size_t pages_workspace_bytes(int n_pages)
+{
+    const size_t n = n_pages > CONFU_MAX_PAGE_REQUESTS ? n_pages : CONFU_MAX_PAGE_REQUESTS;
+    return 256 + align_up(n * sizeof(int2), 256) + align_up((size_t)n_pages * sizeof(int32_t), 256);
+}
+
+cudaError_t launch_pages_reserve(const confu_pages& pg, int n, const int32_t* rows, const int32_t* lengths, int32_t* status, cudaStream_t st)
+{
+    return launch_pdl(pages_reserve_kernel, dim3(1), dim3(kThreads), st, pg, n, rows, lengths, status);
+}
+
+cudaError_t launch_pages_fork(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, const confu_pages& pg, int n,
+                              const int32_t* src_rows, const int32_t* dst_rows, const int32_t* lengths, void* workspace, int32_t* status, cudaStream_t st)
+{
+    cudaError_t e = launch_pdl(pages_fork_kernel, dim3(1), dim3(kThreads), st, pg, n, src_rows, dst_rows, lengths, workspace, status);
+    if (e != cudaSuccess) return e;
+    const CopyList c = copy_list(workspace);
+    return copy(ctx, pools_of(ctx, d, n_layers, k_layers, v_layers, pg.n_pages), n, c.count, c.pairs, nullptr, nullptr, nullptr, pg, nullptr, st);
+}
+
+cudaError_t launch_pages_free(const confu_pages& pg, int n, const int32_t* rows, int32_t* status, cudaStream_t st)
+{
+    return launch_pdl(pages_free_kernel, dim3((unsigned)((n + 7) / 8)), dim3(256), st, pg, n, rows, status);
+}
+
+cudaError_t launch_pages_compact(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, const confu_pages& pg,
+                                 int32_t* page_map, int32_t* n_used, void* workspace, cudaStream_t st)
+{
+    if (!page_map) {
+        const size_t n = pg.n_pages > CONFU_MAX_PAGE_REQUESTS ? pg.n_pages : CONFU_MAX_PAGE_REQUESTS;
+        page_map = (int32_t*)((char*)workspace + 256 + align_up(n * sizeof(int2), 256));
+    }
+    cudaError_t e = launch_pdl(pages_map_kernel, dim3(1), dim3(kThreads), st, pg, page_map, n_used, workspace);
+    if (e != cudaSuccess) return e;
+    const CopyList c = copy_list(workspace);
+    return copy(ctx, pools_of(ctx, d, n_layers, k_layers, v_layers, pg.n_pages), pg.n_pages, c.count, c.pairs, nullptr, nullptr, nullptr, pg, page_map, st);
+}
+
+cudaError_t launch_pages_copy(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers, int n_pages, int n,
+                              const int32_t* src_pages, const int32_t* dst_pages, int32_t* status, cudaStream_t st)
+{
+    const confu_pages none = {};
+    return copy(ctx, pools_of(ctx, d, n_layers, k_layers, v_layers, n_pages), n, nullptr, nullptr, src_pages, dst_pages, status, none, nullptr, st);
+}
+
+}  // namespace confu

@@ -99,6 +99,22 @@ struct Reader {
         void* p = memory(sizeof(void*));
         return p ? *static_cast<confu_ctx**>(p) : nullptr;
     }
+    // int32 of a request each; every array of a call has the first one's number of entries
+    int32_t* requests(long long& n)
+    {
+        PyObject* o = next();
+        if (!ok || o == Py_None) return nullptr;
+        const at::Tensor* t = tensor(o);
+        if (!t) return nullptr;
+        if (t->scalar_type() != at::kInt || (n >= 0 && t->numel() != n)) {
+            PyErr_SetString(PyExc_ValueError, "int32 tensors of as many entries as there are requests");
+            ok = false;
+            return nullptr;
+        }
+        n = t->numel();
+        return static_cast<int32_t*>(t->data_ptr());
+    }
+    const confu_pages* pages() { return static_cast<const confu_pages*>(memory(sizeof(confu_pages))); }
     const confu_dims* dims() { return static_cast<const confu_dims*>(memory(sizeof(confu_dims))); }
     // a torch stream, or None for the current one
     void* stream()
@@ -225,6 +241,75 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args)
     END(confu_kv_append(ctx, dims, k_rows, v_rows, k, v, seq_start, prefix_len, st))
 }
 
+// the request arrays give the number of requests
+PyObject* pages_reserve(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    BEGIN
+    confu_ctx* ctx = r.ctx();
+    const confu_pages* pages = r.pages();
+    long long n = -1;
+    auto rows = r.requests(n), lengths = r.requests(n), status = r.requests(n);
+    void* st = r.stream();
+    END(confu_pages_reserve(ctx, pages, n < 0 ? 0 : (int)n, rows, lengths, status, st))
+}
+
+PyObject* pages_fork(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    BEGIN
+    confu_ctx* ctx = r.ctx();
+    const confu_dims* dims = r.dims();
+    const int n_layers = (int)r.integer();
+    auto k = r.as<void*>(), v = r.as<void*>();
+    const confu_pages* pages = r.pages();
+    long long n = -1;
+    auto src = r.requests(n), dst = r.requests(n), lengths = r.requests(n);
+    size_t ws_bytes = 0;
+    void* ws = r.ptr(&ws_bytes);
+    auto status = r.requests(n);
+    void* st = r.stream();
+    END(confu_pages_fork(ctx, dims, n_layers, k, v, pages, n < 0 ? 0 : (int)n, src, dst, lengths, ws, ws_bytes, status, st))
+}
+
+PyObject* pages_free(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    BEGIN
+    confu_ctx* ctx = r.ctx();
+    const confu_pages* pages = r.pages();
+    long long n = -1;
+    auto rows = r.requests(n), status = r.requests(n);
+    void* st = r.stream();
+    END(confu_pages_free(ctx, pages, n < 0 ? 0 : (int)n, rows, status, st))
+}
+
+PyObject* pages_copy(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    BEGIN
+    confu_ctx* ctx = r.ctx();
+    const confu_dims* dims = r.dims();
+    const int n_layers = (int)r.integer();
+    auto k = r.as<void*>(), v = r.as<void*>();
+    const int n_pages = (int)r.integer();
+    long long n = -1;
+    auto src = r.requests(n), dst = r.requests(n), status = r.requests(n);
+    void* st = r.stream();
+    END(confu_pages_copy(ctx, dims, n_layers, k, v, n_pages, n < 0 ? 0 : (int)n, src, dst, status, st))
+}
+
+PyObject* pages_compact(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    BEGIN
+    confu_ctx* ctx = r.ctx();
+    const confu_dims* dims = r.dims();
+    const int n_layers = (int)r.integer();
+    auto k = r.as<void*>(), v = r.as<void*>();
+    const confu_pages* pages = r.pages();
+    auto map = r.as<int32_t>(), used = r.as<int32_t>();
+    size_t ws_bytes = 0;
+    void* ws = r.ptr(&ws_bytes);
+    void* st = r.stream();
+    END(confu_pages_compact(ctx, dims, n_layers, k, v, pages, map, used, ws, ws_bytes, st))
+}
+
 // (host state only, but called before every layer's calls)
 PyObject* set_kv_block_scales(PyObject*, PyObject* const* args, Py_ssize_t n_args)
 {
@@ -260,7 +345,8 @@ PyObject* con_embedding(PyObject*, PyObject* const* args, Py_ssize_t n_args)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(tree_plan), FAST(tree_attention), FAST(tree_accept), FAST(tree_accept_match), FAST(kv_compact),
-                         FAST(kv_append), FAST(set_kv_block_scales), FAST(con_embedding), {nullptr, nullptr, 0, nullptr}};
+                         FAST(kv_append), FAST(set_kv_block_scales),
+                         FAST(pages_reserve), FAST(pages_fork), FAST(pages_free), FAST(pages_copy), FAST(pages_compact), FAST(con_embedding), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
