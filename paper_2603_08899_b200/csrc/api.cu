@@ -83,6 +83,10 @@ cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const vo
                                    const void* v_cache, int64_t n_slots, const SlotMap& map, const int32_t* prefix_len,
                                    const void* k_soft, const void* v_soft, const void* plan, void* partials, void* out,
                                    float* lse, int32_t* status, cudaStream_t st);
+cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache,
+                                      const void* v_cache, int64_t n_slots, const SlotMap& map, const int32_t* prefix_len,
+                                      const void* k_soft, const void* v_soft, const void* plan, void* partials, void* out,
+                                      float* lse, int32_t* status, cudaStream_t st);
 cudaError_t launch_append_block(const Ctx* ctx, const confu_dims& d, const void* k_rows, const void* v_rows, void* k_cache,
                                 void* v_cache, const SlotMap& map, const int32_t* prefix_len, cudaStream_t st);
 cudaError_t launch_compact_block(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers,
@@ -107,6 +111,9 @@ cudaError_t launch_attention_tc(const Ctx* ctx, const confu_dims& d, const void*
 
 namespace {
 
+// Rows of a kv head up to which a block-scaled cache is read by the kernel that keeps keys and values in registers.
+constexpr int kBlockRegisterRows = 32;
+
 // Which attention kernel serves these dims under the context's option: a CONFU_ATTENTION_* value
 // (never _AUTO, nor _TENSOR_NARROW, see plan_kind), or a negative error code when a forced path cannot take them.
 int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
@@ -120,8 +127,10 @@ int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
         return ok && fp8_attention_supported(d) && ctx->sm_count >= n_rg ? (int)CONFU_ATTENTION_TENSOR : (int)CONFU_ERR_UNSUPPORTED;
     }
     if (d.kv_dtype == CONFU_FP8_BLOCK) {
-        const bool ok = ctx->attention_path == CONFU_ATTENTION_AUTO || ctx->attention_path == CONFU_ATTENTION_GENERIC;
-        return ok && ctx->sm_count >= n_rg ? (int)CONFU_ATTENTION_GENERIC : (int)CONFU_ERR_UNSUPPORTED;
+        if (ctx->attention_path == CONFU_ATTENTION_TENSOR_PAIR || ctx->sm_count < n_rg) return CONFU_ERR_UNSUPPORTED;
+        if (ctx->attention_path != CONFU_ATTENTION_AUTO) return ctx->attention_path;
+        const int rows = (d.T + d.C) * (d.Hq / d.Hkv);
+        return rows <= kBlockRegisterRows ? CONFU_ATTENTION_GENERIC : CONFU_ATTENTION_TENSOR;
     }
     switch (ctx->attention_path) {
         case CONFU_ATTENTION_GENERIC: return CONFU_ATTENTION_GENERIC;
@@ -370,7 +379,7 @@ int confu_tree_attention(confu_ctx* ctx, const confu_dims* dims, const void* q, 
     }
     cudaError_t e;
     if (dims->kv_dtype == CONFU_FP8_BLOCK)
-        e = launch_attention_block(ctx, *dims, q, k_cache, v_cache, n_slots, map, prefix_len, k_soft, v_soft, use_plan,
+        e = (path == CONFU_ATTENTION_TENSOR ? launch_attention_block_tc : launch_attention_block)(ctx, *dims, q, k_cache, v_cache, n_slots, map, prefix_len, k_soft, v_soft, use_plan,
                                    ws + ws_partial_offset(dims), out, lse, status, st);
     else if (path == CONFU_ATTENTION_TENSOR_PAIR)
         e = launch_attention_pair(ctx, *dims, q, k_cache, v_cache, n_slots, map, prefix_len, k_soft, v_soft,

@@ -106,7 +106,7 @@ def compare(case, got, sm_scale=None, what=""):
     assert worst <= 1, f"{what}: lse {worst} times the tolerance"
 
 
-PATHS = [cb.ATTENTION_AUTO, cb.ATTENTION_GENERIC]
+PATHS = [cb.ATTENTION_AUTO, cb.ATTENTION_GENERIC, cb.ATTENTION_TENSOR]
 ATTEND = {
     "one_token": dict(T=1, C=0, S=0),
     "one_token_no_prefix": dict(T=1, C=0, S=0, prefix=[0, 1, 2]),
