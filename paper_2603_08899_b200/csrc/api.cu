@@ -66,6 +66,7 @@ cudaError_t launch_bounded_wait(unsigned long long limit_ns, int32_t* status, cu
 bool tc_attention_supported(const confu_dims& d);
 bool pair_attention_supported(const confu_dims& d);
 bool fp8_attention_supported(const confu_dims& d);
+bool block_register_supported(const confu_dims& d);
 cudaError_t launch_attention_fp8(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache,
                                  const void* v_cache, int64_t n_slots, const SlotMap& map,
                                  const int32_t* prefix_len, const void* k_soft, const void* v_soft, const void* plan,
@@ -111,9 +112,6 @@ cudaError_t launch_attention_tc(const Ctx* ctx, const confu_dims& d, const void*
 
 namespace {
 
-// Rows of a kv head up to which a block-scaled cache is read by the kernel that keeps keys and values in registers.
-constexpr int kBlockRegisterRows = 32;
-
 // Which attention kernel serves these dims under the context's option: a CONFU_ATTENTION_* value
 // (never _AUTO, nor _TENSOR_NARROW, see plan_kind), or a negative error code when a forced path cannot take them.
 int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
@@ -127,10 +125,9 @@ int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
         return ok && fp8_attention_supported(d) && ctx->sm_count >= n_rg ? (int)CONFU_ATTENTION_TENSOR : (int)CONFU_ERR_UNSUPPORTED;
     }
     if (d.kv_dtype == CONFU_FP8_BLOCK) {
-        if (ctx->attention_path == CONFU_ATTENTION_TENSOR_PAIR || ctx->sm_count < n_rg) return CONFU_ERR_UNSUPPORTED;
-        if (ctx->attention_path != CONFU_ATTENTION_AUTO) return ctx->attention_path;
-        const int rows = (d.T + d.C) * (d.Hq / d.Hkv);
-        return rows <= kBlockRegisterRows ? CONFU_ATTENTION_GENERIC : CONFU_ATTENTION_TENSOR;
+        const int path = ctx->attention_path != CONFU_ATTENTION_AUTO ? ctx->attention_path : block_register_supported(d) ? (int)CONFU_ATTENTION_GENERIC : (int)CONFU_ATTENTION_TENSOR;
+        const bool ok = path == CONFU_ATTENTION_TENSOR || (path == CONFU_ATTENTION_GENERIC && block_register_supported(d));
+        return ok && ctx->sm_count >= n_rg ? path : (int)CONFU_ERR_UNSUPPORTED;
     }
     switch (ctx->attention_path) {
         case CONFU_ATTENTION_GENERIC: return CONFU_ATTENTION_GENERIC;

@@ -81,8 +81,13 @@ def test_dims_and_paths(ctx):
         assert cb.lib().confu_plan_bytes(C.byref(ctx), C.byref(dims(**kw))) > 0
     ctx.attention_path = cb.ATTENTION_TENSOR_PAIR
     assert path() == UNSUPPORTED
-    ctx.attention_path = cb.ATTENTION_GENERIC
-    assert path() == cb.ATTENTION_GENERIC
+    few, many = dict(T=8, Cn=0), dict(T=9, Cn=0)                     # 32 and 36 rows x heads of a kv head
+    for option, a, b in ((cb.ATTENTION_AUTO, cb.ATTENTION_GENERIC, cb.ATTENTION_TENSOR), (cb.ATTENTION_GENERIC, cb.ATTENTION_GENERIC, UNSUPPORTED),
+                         (cb.ATTENTION_TENSOR, cb.ATTENTION_TENSOR, cb.ATTENTION_TENSOR)):
+        ctx.attention_path = option
+        assert path(**few) == a and path(**many) == b
+    ctx.attention_path, ctx.sm_count = cb.ATTENTION_AUTO, 1          # a share is walked by a CTA per group of query rows
+    assert path(T=64, Cn=64) == UNSUPPORTED and path(**many) == cb.ATTENTION_TENSOR
 
 
 def attention(ctx, d, table=True, soft=None, ws=1 << 40, n_slots=1280, q=AT):
