@@ -9,7 +9,7 @@
 //     Rows past the last slot, and pages outside the pool, are written as zeros.
 //   - the scales of a tile go with its K, through shared memory, as {ks, log2 vs, 1 / vs} of every 32 keys: a thread's row has one factor
 //     and one addend of the exponent's argument per 32 keys;
-//   - q is turned into f16 by the softmax threads, a row each, scaled by the power of two that brings the row's largest magnitude into [1, 2).
+//   - q is turned into f16 in its place in shared memory by the softmax threads, a row each, scaled by the power of two that brings the row's largest magnitude into [1, 2).
 //
 // For whole trees (rows x heads of a kv head > 32): the products bind, 256 FLOP per byte of a bf16 cache and twice that here.
 #include "e4m3.cuh"
@@ -18,14 +18,19 @@
 namespace confu {
 
 namespace tc {
+
+bool make_tile_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t box_rows, uint32_t box_heads, uint32_t head_dim);
+
 namespace blktc {
 
-constexpr int kThreads = 512;            // warps 0-3: softmax of M tile 0, 4-7: of M tile 1, 8-11: codes to f16, 12: MMA
+// warps 0-3: softmax of M tile 0, 4-7: of M tile 1, 8-11: codes to f16, 12: MMA, 13: where the tiles are, 14: Q
+constexpr int kThreads = 512;
 template <int D> constexpr int kTile = kTileKeys * D * 2;             // a 128-key tile as f16
 template <int D> constexpr int kStages = D == 128 ? 2 : 4;            // stage g = [V of the CTA's g-1st key tile | K of its g-th]
 constexpr uint32_t kTmemCols = 512;                 // S0 | S1 | O0 | O1, 128 columns each; P_t overlays S_t
 constexpr float kRescaleThreshold = 8.f;            // weights stay <= 2^8
 constexpr float kLeastScale = 7.8886091e-31f;       // 2^-100
+constexpr int kAhead = 8;                           // tiles that are known ahead of their conversion
 // Scales of a tile are read by the softmax threads until they have handed over its weights.  Tile g + 5 (g + 3 with two stages) is not
 // converted before P V of tile g: a ring of eight is enough.
 constexpr int kScaleRing = 8;
@@ -36,153 +41,182 @@ template <int D> constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | ((uint32_
 struct BlockParams {
     const uint8_t *k, *v, *k_soft, *v_soft;
     const float *ks, *vs, *ks_soft, *vs_soft;
-    const __nv_bfloat16* q;
     int64_t n_pages;
     int block;
 };
 
+struct alignas(16) TileDesc {
+    const uint8_t *k, *v;              // of the tile's first key
+    int valid;                         // keys that exist and can be read; -1: there are no more tiles
+    int pad[3];
+    float4 scales[4];                  // per 32 keys: ks, log2 vs, 1 / vs
+};
+
 template <int D>
 struct SharedStorage {
-    alignas(1024) uint8_t q[2 * kTile<D>];               // two M tiles
+    alignas(1024) uint8_t q[2 * kTile<D>];               // two M tiles: bf16 as they arrive, then f16
     alignas(1024) uint8_t kv[kStages<D>][2][kTile<D>];   // [stage][0: V tile, 1: K tile]
-    alignas(16) float4 scales[kScaleRing][4];            // per 32 keys: ks, log2 vs, 1 / vs
-    alignas(8) uint64_t q_full[2];
+    alignas(16) float4 xpose[8][32 * 8];                 // per softmax warp: a 32 x 32 fp32 tile, as in attn_tc.cu
+    TileDesc tiles[kAhead];
+    float4 scales[kScaleRing][4];
+    alignas(8) uint64_t q_landed, q_empty, q_full[2];
+    uint64_t tile_full[kAhead], tile_empty[kAhead];
     uint64_t kv_full[kStages<D>], kv_empty[kStages<D>];
     uint64_t scales_full[kScaleRing];
     uint64_t s_full[2][2], p_full[2][2], o_done[2];      // [M tile][half of the key tile]
     uint64_t pv0_done[2];                 // P V of half 0 of a run's last tile has completed
     uint32_t tmem_base;
     int abort;
-    alignas(16) float4 xpose[8][32 * 8];                 // per softmax warp: a 32 x 32 fp32 tile, as in attn_tc.cu
 };
 
 // ------------------------------------------------------------------------------------ roles
-struct TileRef {
-    int64_t row;                       // first slot in the pool (soft prompts: 0)
-    int g, valid;                      // kv head; keys of the tile that exist
-    int page;                          // -1: the soft prompts, -2: outside the pool
-};
-
-// The CTA's key tiles in walking order.
-struct TileWalk {
+// One warp walks the CTA's key tiles ahead of everybody and writes down where they are: pages and scales of eight tiles are looked up at once
+// (a lane per 32 keys), so that nobody else waits for a chain of dependent reads.
+template <int D>
+__device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
+{
+    const int lane = threadIdx.x & 31, sub = lane & 3, Hkv = prm.d.Hkv, nb = kTileKeys / bp.block;
     Walker w;
     Segment s;
-    int t;
-    bool run;
-    __device__ void begin(const PlanView& pv, const Params& prm)
-    {
-        run = w.begin(pv, prm, blockIdx.x, kPlanCta, s);
-        t = s.t0;
-    }
-    __device__ bool next(const Params& prm, const BlockParams& bp, TileRef& r)
-    {
-        if (!run) return false;
-        r.g = s.g;
-        if (t >= s.nkt) {
-            r.page = -1;
-            r.row = 0;
-            r.valid = prm.d.S;
-        } else {
-            const int page = __ldg(prm.map.block_table + (size_t)s.b * prm.map.max_pages + t);
-            const int64_t left = s.P + prm.d.T + prm.d.C - (int64_t)t * kTileKeys;
-            r.valid = (int)min(left, (int64_t)kTileKeys);
-            r.page = (uint32_t)page < (uint64_t)bp.n_pages ? page : -2;
-            r.row = (int64_t)page * kTileKeys;
+    uint32_t g = 0;
+    auto put = [&](int j, const TileDesc& d, const float4& scale) -> bool {       // the lanes of tile j of eight
+        const uint32_t e = g % kAhead;
+        if (!__all_sync(0xffffffffu, mbar_wait(&sh.tile_empty[e], ((g / kAhead) & 1) ^ 1, &sh.abort, prm.wait_ns))) return false;
+        if ((lane >> 2) == j) {
+            sh.tiles[e].scales[sub] = scale;
+            if (sub == 0) {
+                sh.tiles[e].k = d.k;
+                sh.tiles[e].v = d.v;
+                sh.tiles[e].valid = d.valid;
+            }
         }
-        if (++t == s.t1) {
-            run = w.next(s);
-            t = s.t0;
-        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.tile_full[e]);
+        ++g;
         return true;
+    };
+    TileDesc d;
+    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s)) {
+        const int32_t* table = prm.map.block_table + (size_t)s.b * prm.map.max_pages;
+        for (int t0 = s.t0; t0 < s.t1; t0 += 8) {
+            const int t = t0 + (lane >> 2);
+            const bool soft = t >= s.nkt;
+            const int page = t < s.t1 && !soft ? __ldg(table + t) : -1;
+            const bool there = t < s.t1 && (soft || (uint32_t)page < (uint64_t)bp.n_pages);
+            const int64_t left = soft ? prm.d.S : s.P + prm.d.T + prm.d.C - (int64_t)t * kTileKeys;
+            const size_t at = ((size_t)(soft || !there ? 0 : page) * kTileKeys * Hkv + s.g) * D;
+            d.valid = there ? (int)min(left, (int64_t)kTileKeys) : 0;
+            d.k = (soft ? bp.k_soft : bp.k) + at;
+            d.v = (soft ? bp.v_soft : bp.v) + at;
+            float ks = 1.f, vs = 1.f;
+            if (sub * 32 < d.valid) {
+                const size_t sc = ((size_t)(soft ? 0 : page) * Hkv + s.g) * nb + sub * 32 / bp.block;
+                ks = __ldg((soft ? bp.ks_soft : bp.ks) + sc);
+                vs = fmaxf(__ldg((soft ? bp.vs_soft : bp.vs) + sc), kLeastScale);
+            }
+            const float4 scale = make_float4(ks, log2f(vs), 1.f / vs, 0.f);
+            for (int j = 0; j < 8 && t0 + j < s.t1; ++j)
+                if (!put(j, d, scale)) return;
+        }
     }
-};
+    d.k = d.v = nullptr;
+    d.valid = -1;
+    put(0, d, make_float4(1.f, 0.f, 1.f, 0.f));
+}
 
-// 16 bytes of a row: thread t has piece t % (D / 16) of rows t / (D / 16), + 2048 / D, ...
+// Q of a run, bf16, as soon as the last product of the run before has read that one's.
+template <int D>
+__device__ void q_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, const CUtensorMap* q_map)
+{
+    Walker w;
+    Segment s;
+    uint32_t seg = 0;
+    const int R = prm.d.T + prm.d.C;
+    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s), ++seg) {
+        if (!mbar_wait(&sh.q_empty, (seg & 1) ^ 1, &sh.abort, prm.wait_ns)) return;
+        mbar_arrive_expect_tx(&sh.q_landed, (D / 64) * prm.n_mt * (uint32_t)(prm.rpt * prm.G) * 128u);
+        for (int mt = 0; mt < prm.n_mt; ++mt)
+            for (int kb = 0; kb < D / 64; ++kb)
+                tma_load_3d(sh.q + mt * kTile<D> + kb * kHalfTile, q_map, &sh.q_landed, kb * 64, s.g * prm.G, s.b * R + prm.rpt * (2 * s.rg + mt));
+    }
+}
+
+// 16 bytes of a row of codes per thread, of a row in every kRows: eight lanes in a row have the same half of two neighbouring rows (D = 128) or
+// two rows (D = 64), so that the swizzled pieces they write meet eight different groups of banks.
 template <int D>
 struct Codes {
     static constexpr int kPieces = D / 16, kRows = 128 / kPieces, n = kTileKeys / kRows;
     uint4 w[n];
-    __device__ __forceinline__ void load(const uint8_t* pool, const TileRef& r, int Hkv, int tid)
+    __device__ __forceinline__ static int row_of(int tid) { return D == 128 ? (tid >> 5) * 4 + ((tid >> 2) & 3) : tid >> 2; }
+    __device__ __forceinline__ static int piece_of(int tid) { return D == 128 ? (tid & 3) + ((tid >> 4) & 1) * 4 : tid & 3; }
+    __device__ __forceinline__ void load(const uint8_t* p, int valid, uint32_t pitch, int tid)
     {
-        const size_t pitch = (size_t)Hkv * D;
-        const uint8_t* p = pool + ((size_t)r.row * Hkv + r.g) * D + (tid / kPieces) * pitch + (tid % kPieces) * 16;
-        const int valid = r.page == -2 ? 0 : r.valid - tid / kPieces;
+        p += row_of(tid) * pitch + piece_of(tid) * 16;
+        valid -= row_of(tid);
 #pragma unroll
         for (int i = 0; i < n; ++i) {
             w[i] = make_uint4(0u, 0u, 0u, 0u);
             if (i * kRows < valid)
                 asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w)
-                             : "l"(p + (size_t)i * kRows * pitch));
+                             : "l"(p));
+            p += (size_t)kRows * pitch;
         }
     }
-    // into [D / 64 halves][128 rows][128 B], 128-byte swizzle.  Lanes of the second half write their two pieces the other way round: eight lanes
-    // then meet eight different groups of banks.
+    // into [D / 64 halves][128 rows][128 B], 128-byte swizzle (kRows is a multiple of 8: it is the same for all of a thread's rows)
     __device__ __forceinline__ void store(uint8_t* tile, int tid) const
     {
-        const int piece = tid % kPieces, half = piece >> 2, c0 = 2 * (piece & 3), first = half;
+        const int piece = piece_of(tid), row = row_of(tid);
+        uint8_t* to = tile + (piece >> 2) * kHalfTile + row * 128 + (((2 * (piece & 3)) ^ (row & 7)) << 4);
+        uint8_t* to1 = reinterpret_cast<uint8_t*>(reinterpret_cast<uintptr_t>(to) ^ 16);
 #pragma unroll
         for (int i = 0; i < n; ++i) {
-            const int row = tid / kPieces + i * kRows;
-            uint4 lo, hi;
-            e4m3_to_f16x4(w[i].x, lo.x, lo.y);
-            e4m3_to_f16x4(w[i].y, lo.z, lo.w);
-            e4m3_to_f16x4(w[i].z, hi.x, hi.y);
-            e4m3_to_f16x4(w[i].w, hi.z, hi.w);
-            uint8_t* to = tile + half * kHalfTile + row * 128;
-            const uint4 a = first ? hi : lo, b = first ? lo : hi;
-            *reinterpret_cast<uint4*>(to + (((c0 + first) ^ (row & 7)) << 4)) = a;
-            *reinterpret_cast<uint4*>(to + (((c0 + 1 - first) ^ (row & 7)) << 4)) = b;
+            uint4 x;
+            e4m3_to_f16x4(w[i].x, x.x, x.y);
+            e4m3_to_f16x4(w[i].y, x.z, x.w);
+            *reinterpret_cast<uint4*>(to + i * kRows * 128) = x;
+            e4m3_to_f16x4(w[i].z, x.x, x.y);
+            e4m3_to_f16x4(w[i].w, x.z, x.w);
+            *reinterpret_cast<uint4*>(to1 + i * kRows * 128) = x;
         }
     }
 };
 
+// Four warps turn the codes of tile after tile into f16, those of the next tile on their way meanwhile.  Stage g of the ring carries V of tile
+// g - 1 and K of tile g.
 template <int D>
-__device__ void convert_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
+__device__ void convert_role(SharedStorage<D>& sh, const Params& prm)
 {
-    const int tid = threadIdx.x & 127, Hkv = prm.d.Hkv, nb = kTileKeys / bp.block;
-    TileWalk walk;
-    walk.begin(pv, prm);
-    TileRef cur, next;                               // tiles g and g + 1 of the walk
-    if (!walk.next(prm, bp, cur)) return;
-    bool have_next = walk.next(prm, bp, next);
+    const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
+    const uint32_t pitch = (uint32_t)prm.d.Hkv * D;
     Codes<D> k, v;
-    float ks = 1.f, vs = 1.f;                        // threads 0-3: of 32 keys of the tile whose K is under way
-    auto load_k = [&](const TileRef& r) {
-        k.load(r.page == -1 ? bp.k_soft : bp.k, r, Hkv, tid);
-        ks = vs = 1.f;
-        if (tid < 4 && tid * 32 < r.valid && r.page != -2) {
-            const size_t at = ((size_t)(r.page == -1 ? 0 : r.page) * Hkv + r.g) * nb + tid * 32 / bp.block;
-            ks = __ldg((r.page == -1 ? bp.ks_soft : bp.ks) + at);
-            vs = __ldg((r.page == -1 ? bp.vs_soft : bp.vs) + at);
-        }
-    };
-    auto load_v = [&](const TileRef& r) { v.load(r.page == -1 ? bp.v_soft : bp.v, r, Hkv, tid); };
-    load_k(cur);
-    load_v(cur);
-    bool have_cur = true;
-    for (uint32_t g = 0;; ++g) {                     // stage g: V of tile g - 1, K of tile g
-        const uint32_t st = g % kStages<D>;
+    if (!mbar_wait(&sh.tile_full[0], 0, &sh.abort, prm.wait_ns)) return;
+    int valid = sh.tiles[0].valid;                   // of tile g; -1: there is none
+    if (valid < 0) return;                           // (nobody waits for a share without tiles)
+    k.load(sh.tiles[0].k, valid, pitch, tid);
+    v.load(sh.tiles[0].v, valid, pitch, tid);
+    for (uint32_t g = 0;; ++g) {
+        const uint32_t st = g % kStages<D>, e = g % kAhead;
         if (!mbar_wait(&sh.kv_empty[st], ((g / kStages<D>) & 1) ^ 1, &sh.abort, prm.wait_ns)) return;
         if (g > 0) {
             v.store(sh.kv[st][0], tid);
-            if (have_cur) load_v(cur);
+            if (valid >= 0) v.load(sh.tiles[e].v, valid, pitch, tid);
         }
-        if (have_cur) {
+        if (valid >= 0) {
             k.store(sh.kv[st][1], tid);
             if (tid < 4) {
-                const float least = fmaxf(vs, kLeastScale);
-                sh.scales[g % kScaleRing][tid] = make_float4(ks, log2f(least), 1.f / least, 0.f);
+                sh.scales[g % kScaleRing][tid] = sh.tiles[e].scales[tid];
                 mbar_arrive(&sh.scales_full[g % kScaleRing]);
             }
-            if (have_next) load_k(next);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.tile_empty[e]);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&sh.kv_full[st]);
-        if (!have_cur) return;
-        cur = next;
-        have_cur = have_next;
-        if (have_next) have_next = walk.next(prm, bp, next);
+        if (valid < 0) return;                       // the last stage: V of the last tile, no K
+        if (!mbar_wait(&sh.tile_full[(g + 1) % kAhead], ((g + 1) / kAhead) & 1, &sh.abort, prm.wait_ns)) return;
+        valid = sh.tiles[(g + 1) % kAhead].valid;
+        if (valid >= 0) k.load(sh.tiles[(g + 1) % kAhead].k, valid, pitch, tid);
     }
 }
 
@@ -252,6 +286,7 @@ __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView
             }
         }
         if (issuer) tc_commit(&sh.kv_empty[st]);
+        if (have_cur && cur_last && issuer) tc_commit(&sh.q_empty);               // the last Q K^T of the run has been issued
         ++stage;
         have_prev = have_cur;
         prev_first = cur_first;
@@ -274,15 +309,16 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return r;
 }
 
-// A row of q -> f16 in the M tile that the tensor pipe reads, divided by 2^e with 2^e <= largest magnitude < 2^(e + 1); returns 2^e.
+// A row of the M tile, bf16 -> f16 in its place, divided by 2^e with 2^e <= largest magnitude < 2^(e + 1); returns 2^e.
 template <int D>
-__device__ __forceinline__ float put_q_row(const __nv_bfloat16* q, bool there, uint8_t* tile, int row)
+__device__ __forceinline__ float convert_q_row(uint8_t* tile, bool there, int row)
 {
     uint4 raw[D / 8];
     float amax = 0.f;
 #pragma unroll
     for (int j = 0; j < D / 8; ++j) {
-        raw[j] = there ? __ldg(reinterpret_cast<const uint4*>(q) + j) : make_uint4(0u, 0u, 0u, 0u);
+        raw[j] = *reinterpret_cast<const uint4*>(tile + (j >> 3) * kHalfTile + row * 128 + (((j & 7) ^ (row & 7)) << 4));
+        if (!there) raw[j] = make_uint4(0u, 0u, 0u, 0u);         // (never written)
         const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -337,7 +373,7 @@ __device__ __forceinline__ float weights32(const uint32_t* sv, float a, float ad
 }
 
 template <int D>
-__device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, uint32_t tmem, int t /*M tile*/)
+__device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem, int t /*M tile*/)
 {
     const int lane_row = threadIdx.x & 127;                 // row of the M tile = TMEM lane
     const int warp_in_wg = (threadIdx.x >> 5) & 3;
@@ -354,8 +390,8 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Bloc
         const int r = prm.rpt * (2 * s.rg + t) + lane_row / G;            // query row of this thread in this pair
         const bool row_valid = lane_row < prm.rpt * G && r < R;
         const uint64_t mask = row_valid ? pv.mask[(size_t)s.b * kMaxRows + r] : 0ull;
-        // (every Q K^T of the run before has completed: this thread has seen its last scores)
-        const float q_scale = put_q_row<D>(bp.q + (((size_t)s.b * R + (row_valid ? r : 0)) * Hq + s.g * G + hl) * D, row_valid, sh.q + t * kTile<D>, lane_row);
+        if (!mbar_wait(&sh.q_landed, seg & 1, &sh.abort, prm.wait_ns)) return;
+        const float q_scale = convert_q_row<D>(sh.q + t * kTile<D>, row_valid, lane_row);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&sh.q_full[t]);
         const float c = prm.c * q_scale;
@@ -408,10 +444,11 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Bloc
                 }
                 // P over the columns of the half (whose scores sit in registers by now); masked scores get weight exactly 0
                 const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
-                uint32_t pk[32];
+                uint32_t pk[16];
                 l = fmaf(weights32(sv, a0, sc0.y + neg_m, pk), sc0.z, l);
-                l = fmaf(weights32(sv + 32, a1, sc1.y + neg_m, pk + 16), sc1.z, l);
-                tmem_st32(s_addr + h * 64, pk);
+                tmem_st16(s_addr + h * 64, pk);
+                l = fmaf(weights32(sv + 32, a1, sc1.y + neg_m, pk), sc1.z, l);
+                tmem_st16(s_addr + h * 64 + 16, pk);
                 tc_wait_st();
                 tc_fence_before();
                 mbar_arrive(&sh.p_full[t][h]);
@@ -484,15 +521,18 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Bloc
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const Params prm, const BlockParams bp)
+__global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const __grid_constant__ CUtensorMap q_map, const Params prm, const BlockParams bp)
 {
     extern __shared__ uint8_t smem_raw[];
     SharedStorage<D>& sh = *reinterpret_cast<SharedStorage<D>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5;
 
     if (threadIdx.x == 0) {
+        mbar_init(&sh.q_landed, 1);
+        mbar_init(&sh.q_empty, 1);
         // a stage is full when every converting thread has written its pieces, free again when its MMAs have completed
         for (int i = 0; i < kStages<D>; ++i) { mbar_init(&sh.kv_full[i], 128); mbar_init(&sh.kv_empty[i], 1); }
+        for (int i = 0; i < kAhead; ++i) { mbar_init(&sh.tile_full[i], 1); mbar_init(&sh.tile_empty[i], 4); }
         for (int i = 0; i < kScaleRing; ++i) mbar_init(&sh.scales_full[i], 4);
         for (int t = 0; t < 2; ++t) {
             mbar_init(&sh.q_full[t], 128);
@@ -524,15 +564,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const P
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int t = warp >> 2;
-        if (t < prm.n_mt) softmax_role<D>(sh, prm, bp, pv, tmem, t);
+        if (t < prm.n_mt) softmax_role<D>(sh, prm, pv, tmem, t);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-        convert_role<D>(sh, prm, bp, pv);
+        convert_role<D>(sh, prm);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 12) {
             if (prm.n_mt > 1) mma_role<D, true>(sh, prm, pv, tmem);
             else mma_role<D, false>(sh, prm, pv, tmem);
+        } else if (warp == 13)
+            tiles_role<D>(sh, prm, bp, pv);
+        else if (warp == 14) {
+            if ((threadIdx.x & 31) == 0) q_role<D>(sh, prm, pv, &q_map);
         }
         __syncwarp();
     }
@@ -540,6 +584,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const P
     tc_fence_before();
     __syncthreads();
     if (sh.abort) {
+        // give copies that may still be in flight time to land before the CTA's shared memory goes away
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 200000ull) __nanosleep(1000);
         if (threadIdx.x == 0 && prm.status)
             for (int b = 0; b < prm.d.B; ++b) prm.status[b] = CONFU_ST_TIMEOUT;
         __syncthreads();
@@ -551,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const P
 }
 
 template <int D>
-cudaError_t launch(const Params& prm, const BlockParams& bp, int units, cudaStream_t st)
+cudaError_t launch(const CUtensorMap& q_map, const Params& prm, const BlockParams& bp, int units, cudaStream_t st)
 {
     const size_t smem = sizeof(SharedStorage<D>) + 1024;
     static OncePerDevice attr_done;
@@ -567,7 +614,7 @@ cudaError_t launch(const Params& prm, const BlockParams& bp, int units, cudaStre
     cfg.stream = st;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_block_tc_kernel<D>, prm, bp);
+    return cudaLaunchKernelEx(&cfg, attention_block_tc_kernel<D>, q_map, prm, bp);
 }
 
 }  // namespace blktc
@@ -601,10 +648,11 @@ cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const
     bp.vs = ctx->v_block_scale;
     bp.ks_soft = ctx->k_soft_scale;
     bp.vs_soft = ctx->v_soft_scale;
-    bp.q = (const __nv_bfloat16*)q;
     bp.n_pages = n_slots / kTileKeys;
     bp.block = ctx->block;
-    const cudaError_t e = d.D == 64 ? blktc::launch<64>(prm, bp, ctx->sm_count, st) : blktc::launch<128>(prm, bp, ctx->sm_count, st);
+    CUtensorMap q_map;
+    if (!make_tile_map(&q_map, q, (uint64_t)d.B * (d.T + d.C), d.Hq, prm.rpt, prm.G, d.D)) return cudaErrorInvalidValue;
+    const cudaError_t e = d.D == 64 ? blktc::launch<64>(q_map, prm, bp, ctx->sm_count, st) : blktc::launch<128>(q_map, prm, bp, ctx->sm_count, st);
     if (e != cudaSuccess) return e;
     return launch_combine(prm, ctx->sm_count, st);
 }
