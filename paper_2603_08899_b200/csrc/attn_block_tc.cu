@@ -20,6 +20,7 @@ namespace confu {
 namespace tc {
 
 bool make_tile_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t box_rows, uint32_t box_heads, uint32_t head_dim);
+bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t head_dim);
 
 namespace blktc {
 
@@ -48,7 +49,8 @@ struct BlockParams {
 struct alignas(16) TileDesc {
     const uint8_t *k, *v;              // of the tile's first key
     int valid;                         // keys that exist and can be read; -1: there are no more tiles
-    int pad[3];
+    int g, z;                          // kv head, first slot (-1: not in the pool)
+    int pad;
     float4 scales[4];                  // per 32 keys: ks, log2 vs, 1 / vs
 };
 
@@ -73,7 +75,7 @@ struct SharedStorage {
 // One warp walks the CTA's key tiles ahead of everybody and writes down where they are: pages and scales of eight tiles are looked up at once
 // (a lane per 32 keys), so that nobody else waits for a chain of dependent reads.
 template <int D>
-__device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
+__device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, const CUtensorMap* k_map, const CUtensorMap* v_map)
 {
     const int lane = threadIdx.x & 31, sub = lane & 3, Hkv = prm.d.Hkv, nb = kTileKeys / bp.block;
     Walker w;
@@ -88,6 +90,10 @@ __device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockP
                 sh.tiles[e].k = d.k;
                 sh.tiles[e].v = d.v;
                 sh.tiles[e].valid = d.valid;
+                if (d.z >= 0) {
+                    tma_prefetch_3d(k_map, 0, d.g, d.z);
+                    tma_prefetch_3d(v_map, 0, d.g, d.z);
+                }
             }
         }
         __syncwarp();
@@ -108,6 +114,8 @@ __device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockP
             d.valid = there ? (int)min(left, (int64_t)kTileKeys) : 0;
             d.k = (soft ? bp.k_soft : bp.k) + at;
             d.v = (soft ? bp.v_soft : bp.v) + at;
+            d.g = s.g;
+            d.z = there && !soft ? page * kTileKeys : -1;
             float ks = 1.f, vs = 1.f;
             if (sub * 32 < d.valid) {
                 const size_t sc = ((size_t)(soft ? 0 : page) * Hkv + s.g) * nb + sub * 32 / bp.block;
@@ -120,7 +128,7 @@ __device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockP
         }
     }
     d.k = d.v = nullptr;
-    d.valid = -1;
+    d.valid = d.z = -1;
     put(0, d, make_float4(1.f, 0.f, 1.f, 0.f));
 }
 
@@ -521,7 +529,8 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Plan
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const __grid_constant__ CUtensorMap q_map, const Params prm, const BlockParams bp)
+__global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                          const Params prm, const BlockParams bp)
 {
     extern __shared__ uint8_t smem_raw[];
     SharedStorage<D>& sh = *reinterpret_cast<SharedStorage<D>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -574,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
             if (prm.n_mt > 1) mma_role<D, true>(sh, prm, pv, tmem);
             else mma_role<D, false>(sh, prm, pv, tmem);
         } else if (warp == 13)
-            tiles_role<D>(sh, prm, bp, pv);
+            tiles_role<D>(sh, prm, bp, pv, &k_map, &v_map);
         else if (warp == 14) {
             if ((threadIdx.x & 31) == 0) q_role<D>(sh, prm, pv, &q_map);
         }
@@ -598,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
 }
 
 template <int D>
-cudaError_t launch(const CUtensorMap& q_map, const Params& prm, const BlockParams& bp, int units, cudaStream_t st)
+cudaError_t launch(const CUtensorMap (&maps)[3], const Params& prm, const BlockParams& bp, int units, cudaStream_t st)
 {
     const size_t smem = sizeof(SharedStorage<D>) + 1024;
     static OncePerDevice attr_done;
@@ -614,7 +623,7 @@ cudaError_t launch(const CUtensorMap& q_map, const Params& prm, const BlockParam
     cfg.stream = st;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_block_tc_kernel<D>, q_map, prm, bp);
+    return cudaLaunchKernelEx(&cfg, attention_block_tc_kernel<D>, maps[0], maps[1], maps[2], prm, bp);
 }
 
 }  // namespace blktc
@@ -650,9 +659,11 @@ cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const
     bp.vs_soft = ctx->v_soft_scale;
     bp.n_pages = n_slots / kTileKeys;
     bp.block = ctx->block;
-    CUtensorMap q_map;
-    if (!make_tile_map(&q_map, q, (uint64_t)d.B * (d.T + d.C), d.Hq, prm.rpt, prm.G, d.D)) return cudaErrorInvalidValue;
-    const cudaError_t e = d.D == 64 ? blktc::launch<64>(q_map, prm, bp, ctx->sm_count, st) : blktc::launch<128>(q_map, prm, bp, ctx->sm_count, st);
+    CUtensorMap maps[3];
+    if (!make_tile_map(&maps[0], q, (uint64_t)d.B * (d.T + d.C), d.Hq, prm.rpt, prm.G, d.D) || !make_code_map(&maps[1], k_cache, n_slots, d.Hkv, d.D) ||
+        !make_code_map(&maps[2], v_cache, n_slots, d.Hkv, d.D))
+        return cudaErrorInvalidValue;
+    const cudaError_t e = d.D == 64 ? blktc::launch<64>(maps, prm, bp, ctx->sm_count, st) : blktc::launch<128>(maps, prm, bp, ctx->sm_count, st);
     if (e != cudaSuccess) return e;
     return launch_combine(prm, ctx->sm_count, st);
 }
