@@ -9,15 +9,14 @@
 // 2^-17 of it: nothing else is rounded.
 //
 // Up to 32 rows (query rows x heads of a kv head): reading the cache binds, 2 D bytes a key, and what counts is how many
-// bytes are on their way.  One CTA per SM walks its share of key tiles; one warp keeps a ring of tiles (K and V codes, 32 KB at D = 128)
-// filled by TMA, across the ends of runs; groups of four warps take a tile each in turn, a warp 32 keys of it.  (Codes loaded straight
-// into the registers that the products read, 8 KB a warp under way: 64 sequences of 100..8192, one row, 203 us a layer at 2.8 TB/s, the
-// warps waiting for their loads half of the time.)
+// bytes are on their way.  One CTA per SM walks its share of key tiles in chunks of 32 keys, which 12 warps (8 for more than 16 rows) take in turn.
+// Every warp has a ring of two chunks of its own (K and V codes, 8 KB at D = 128); the lanes of one warp keep them filled by TMA, across the ends of
+// runs, another warp lays out the next run's Q.  (Codes loaded straight into the registers that the products read, 8 KB a warp
+// under way: 64 sequences of 100..8192, one row, 203 us a layer at 2.8 TB/s, the warps waiting for their loads half of the time.)
 //   S = Q K^T    a lane's fragment of K^T is 16 contiguous bytes of a key (the head dims of a product's 16 steps are whatever
 //                bytes the lane has; Q's fragments are laid out in shared memory to match)
 //   O += P V     keys in pairs: a lane has the same 16 columns of two neighbouring keys, byte permutes pair them up
-// Both read the swizzled tile 16 bytes a lane without meeting a bank twice.  The warps meet at the end of a run: sums at the rows' common maximum,
-// group by group through one buffer, in a fixed order.  The plan, its shares and the merge of split pairs are those of the two-M-tile
+// Both read the swizzled tile 16 bytes a lane without meeting a bank twice.  The warps meet at the end of a run, in a fixed order.  The plan, its shares and the merge of split pairs are those of the two-M-tile
 // kernel (attn_tc.cu).  mma.sync and not tcgen05: 16 rows fill its M, an eighth of a tcgen05 tile, and fragments need no second trip through
 // shared memory as f16.
 //
@@ -30,7 +29,7 @@
 namespace confu {
 namespace tc {
 
-bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t head_dim);
+bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t box_rows, uint32_t head_dim);
 
 namespace blk {
 
@@ -45,20 +44,45 @@ struct BlockParams {
     int block;
 };
 
-// kMt M tiles of 16 rows, kGroups groups of four consumer warps
-template <int D, int kMt, int kGroups>
+// kMt M tiles of 16 rows, kWarps consumer warps
+template <int D, int kMt_, int kWarps_>
 struct SharedStorage {
-    static constexpr int kTile = kTileKeys * D;      // codes of a tile
-    static constexpr int kStages = D == 64 ? 8 : kMt == 1 ? 5 : 4;
-    static constexpr int kWarps = 4 * kGroups, kThreads = (kWarps + 4) * 32;      // (and a warpgroup of which one warp fills the ring)
+    static constexpr int kMt = kMt_, kWarps = kWarps_, kThreads = (kWarps + 4) * 32;      // (and a warpgroup that looks after the rings and Q)
+    static constexpr int kCodes = kChunk * D;        // codes of a chunk's K or V
+    static constexpr int kSlots = D == 64 ? 4 : 2;   // of a warp
     // a row of sums: a lane's D / 4 columns apart by 4 floats, rows by 16 banks, so that a warp's 16-byte accesses meet no bank twice
     static constexpr int kSeg = D / 4 + 4, kPitch = 4 * kSeg;
-    alignas(1024) uint8_t kv[kStages][2][kTile];     // [stage][0: K, 1: V]
+    static constexpr int kRowsAtOnce = kMt == 1 ? 4 : 16;      // rows that the warps bring together at a time
+    alignas(1024) uint8_t kv[kWarps][kSlots][2][kCodes];       // [0: K, 1: V]
     alignas(16) uint4 q[kMt][D / 16][32];            // fragments: [M tile][step][lane]
-    alignas(16) float sums[4][kMt * 16][kPitch];     // [quarter of a tile][row]
-    float2 stat[kWarps][kMt * 16];                   // m, l
-    alignas(8) uint64_t full[kStages], empty[kStages];
+    alignas(16) float sums[kWarps][kRowsAtOnce][kPitch];
+    float4 scales[kWarps][kSlots];                   // ks, log2 vs, 1 / vs
+    float2 stat[kWarps][kRowsAtOnce];                // m, l
+    float q_scale[kMt * 16];
+    uint64_t mask[kMt * 16];
+    alignas(8) uint64_t full[kWarps][kSlots], empty[kWarps][kSlots], q_full, q_empty, met;
     int abort;
+};
+
+// The chunks of a run that hold keys: those of its key tiles up to the last slot, then those of the soft prompts.
+struct Chunks {
+    int n_keys, n;
+    __device__ __forceinline__ Chunks(const Segment& s, int keys, int S)
+    {
+        n_keys = max(min(4 * min(s.t1, s.nkt), (keys + kChunk - 1) / kChunk) - 4 * s.t0, 0);
+        n = n_keys + (s.t1 > s.nkt ? (S + kChunk - 1) / kChunk : 0);
+    }
+    // tile and quarter of chunk j
+    __device__ __forceinline__ int tile(const Segment& s, int j) const { return j < n_keys ? s.t0 + (j >> 2) : s.nkt; }
+    __device__ __forceinline__ int sub(int j) const { return j < n_keys ? j & 3 : j - n_keys; }
+};
+
+// Chunk number i of the CTA's walk is warp i % kWarps's, in its slot (i / kWarps) % kSlots.  (A ring of its own for every warp: whoever waits for a
+// phase of a barrier has waited for every phase before it, as a wait on a phase's parity needs.)
+template <typename Sh> struct Place {
+    int warp, slot;
+    uint32_t parity;
+    __device__ __forceinline__ explicit Place(uint32_t i) : warp((int)(i % Sh::kWarps)), slot((int)(i / Sh::kWarps % Sh::kSlots)), parity(i / (Sh::kWarps * Sh::kSlots) & 1) {}
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1)
@@ -74,82 +98,75 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return r;
 }
 
-// Fills the ring: tile after tile of the CTA's share, K and V together.
-template <int D, int kMt, int kGroups>
-__device__ void producer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, const CUtensorMap* k_map,
-                              const CUtensorMap* v_map, const CUtensorMap* ks_map, const CUtensorMap* vs_map)
+// Fills the rings, a lane for each: K and V of the warp's chunks of the share, one after the other, and their scales.  The page of a chunk is looked up
+// two chunks ahead, its scales one.  (One lane for all rings, in order: 64 sequences of 100..8192 165 us a layer, 136 without any arithmetic on
+// the keys; the loop of that lane was what bound.)
+template <int D, typename Sh>
+__device__ void fetch_role(Sh& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, const CUtensorMap* k_map, const CUtensorMap* v_map,
+                           const CUtensorMap* ks_map, const CUtensorMap* vs_map)
 {
-    using Sh = SharedStorage<D, kMt, kGroups>;
-    const int lane = threadIdx.x & 31;
+    const int ring = threadIdx.x & 31, nb = kTileKeys / bp.block;
+    if (ring >= Sh::kWarps) return;
     Walker w;
     Segment s;
-    uint32_t i = 0;
+    uint32_t i0 = 0;
     for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s)) {
+        const Chunks ch(s, (int)s.P + prm.d.T + prm.d.C, prm.d.S);
         const int32_t* table = prm.map.block_table + (size_t)s.b * prm.map.max_pages;
-        int pages = 0, base = s.t0 - 32;
-        for (int t = s.t0; t < s.t1; ++t, ++i) {
-            const bool soft = t >= s.nkt;
-            if (t - base >= 32) {                    // a lane's page of 32 tiles
-                base = t;
-                pages = t + lane < min(s.t1, s.nkt) ? __ldg(table + t + lane) : -1;
-            }
-            const int page = __shfl_sync(0xffffffffu, pages, t - base);
-            const uint32_t st = i % Sh::kStages;
-            const bool ok = mbar_wait(&sh.empty[st], ((i / Sh::kStages) & 1) ^ 1, &sh.abort, prm.wait_ns);
-            if (!__all_sync(0xffffffffu, ok)) return;
-            if (lane == 0) {
-                // (outside the pool: a box that lies before it reads as zeros)
-                const int z = soft ? 0 : (uint32_t)page < (uint64_t)bp.n_pages ? page * kTileKeys : -kTileKeys;
-                mbar_arrive_expect_tx(&sh.full[st], 2 * Sh::kTile);
-                tma_load_3d(sh.kv[st][0], soft ? ks_map : k_map, &sh.full[st], 0, s.g, z);
-                tma_load_3d(sh.kv[st][1], soft ? vs_map : v_map, &sh.full[st], 0, s.g, z);
-            }
+        // (soft prompts have scales like a page's; -1: outside the pool, or no such chunk)
+        auto page_of = [&](int j) -> int { return j < ch.n_keys ? __ldg(table + s.t0 + (j >> 2)) : j < ch.n ? 0 : -1; };
+        auto scales_of = [&](int j, int page) -> float2 {
+            if ((uint32_t)page >= (uint64_t)bp.n_pages) return make_float2(1.f, 1.f);
+            const size_t at = ((size_t)page * prm.d.Hkv + s.g) * nb + ch.sub(j) * kChunk / bp.block;
+            const bool soft = j >= ch.n_keys;
+            return make_float2(__ldg((soft ? bp.ks_soft : bp.ks) + at), __ldg((soft ? bp.vs_soft : bp.vs) + at));
+        };
+        int j = (ring + Sh::kWarps - (int)(i0 % Sh::kWarps)) % Sh::kWarps;
+        int page = page_of(j), page_next = page_of(j + Sh::kWarps);
+        float2 scale = scales_of(j, page);
+        for (; j < ch.n; j += Sh::kWarps) {
+            const int page_after = page_of(j + 2 * Sh::kWarps);
+            const float2 scale_next = scales_of(j + Sh::kWarps, page_next);
+            const Place<Sh> at(i0 + (uint32_t)j);
+            if (!mbar_wait(&sh.empty[ring][at.slot], at.parity ^ 1, &sh.abort, prm.wait_ns)) return;
+            const bool soft = j >= ch.n_keys;
+            const float vs = fmaxf(scale.y, kLeastScale);
+            sh.scales[ring][at.slot] = make_float4(scale.x, log2f(vs), 1.f / vs, 0.f);
+            // (outside the pool: a box that lies before it reads as zeros)
+            const int z = soft ? ch.sub(j) * kChunk : (uint32_t)page < (uint64_t)bp.n_pages ? page * kTileKeys + (j & 3) * kChunk : -kTileKeys;
+            uint64_t* full = &sh.full[ring][at.slot];
+            mbar_arrive_expect_tx(full, 2 * Sh::kCodes);
+            tma_load_3d(sh.kv[ring][at.slot][0], soft ? ks_map : k_map, full, 0, s.g, z);
+            tma_load_3d(sh.kv[ring][at.slot][1], soft ? vs_map : v_map, full, 0, s.g, z);
+            page = page_next;
+            page_next = page_after;
+            scale = scale_next;
         }
+        i0 += (uint32_t)ch.n;
     }
 }
 
-template <int D, int kMt, int kGroups>
-__device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
+// Q of a run, while the run before it is walked: rows of the group, head by head; row m of it is query row r0 + m / G, head m % G of the kv head's.
+template <int D, typename Sh>
+__device__ void q_role(Sh& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
 {
-    using Sh = SharedStorage<D, kMt, kGroups>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp >> 2, sub = warp & 3;
-    const int n = lane >> 2, x = lane & 3;
-    const int G = prm.G, T = prm.d.T, R = prm.d.T + prm.d.C, S = prm.d.S, Hq = prm.d.Hq, Hkv = prm.d.Hkv;
-    const int nb = kTileKeys / bp.block, sub_block = sub * kChunk / bp.block;
-    // bytes of a lane's pieces in a tile.  K: key row 32 sub + 8 t + n, pieces 2 x and 2 x + 1 (D = 64: piece x); V: key rows 32 sub + 8 t + 2 x + o,
-    // the D / 8 bytes from n * D / 8 on.
-    uint32_t k_at[D / 64], v_at[2];
-    if constexpr (D == 128) {
-        k_at[0] = (uint32_t)((sub * kChunk + n) * 128 + (((2 * x) ^ n) << 4));
-        k_at[D / 64 - 1] = (uint32_t)((sub * kChunk + n) * 128 + (((2 * x + 1) ^ n) << 4));
-    } else
-        k_at[0] = (uint32_t)((sub * kChunk + n) * 64 + ((x ^ (n >> 1)) << 4));
-#pragma unroll
-    for (int o = 0; o < 2; ++o)
-        v_at[o] = D == 128 ? (uint32_t)((sub * kChunk + 2 * x + o) * 128 + ((n ^ (2 * x + o)) << 4))
-                           : (uint32_t)((sub * kChunk + 2 * x + o) * 64 + (((n >> 1) ^ x) << 4) + (n & 1) * 8);
-    auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(Sh::kWarps * 32) : "memory"); };
-
+    const int lane = threadIdx.x & 31, n = lane >> 2, x = lane & 3;
+    const int G = prm.G, R = prm.d.T + prm.d.C, Hq = prm.d.Hq;
     Walker w;
-    Segment s, ahead;
-    bool ok = true;
-    uint32_t i0 = 0;                                 // tiles of the runs before
-    bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s);
-    while (run) {
-        const bool more = w.next(ahead);             // (read now: it is there when this run ends)
-        // ---- Q: rows of this group, head by head; row m of it is query row r0 + m / G, head m % G of the kv head's ----
+    Segment s;
+    uint32_t seg = 0;
+    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s), ++seg) {
         const int r0 = prm.rpt * prm.tpg * s.rg, n_rows = min(R - r0, prm.rpt * prm.tpg) * G;
-        float q_scale[kMt][2];                       // of the lane's rows n and n + 8 of an M tile
-        int row_r[kMt][2];                           // their query rows, -1: none
-#pragma unroll
-        for (int mt = 0; mt < kMt; ++mt) {
-            uint32_t raw[2][D / 16][2];              // the lane's bf16 of both rows: steps of four
+#pragma unroll 1
+        for (int mt = 0; mt < Sh::kMt; ++mt) {
+            uint32_t raw[2][D / 16][2];              // the lane's bf16 of rows n and n + 8: steps of four
+            float scale[2];
+            uint64_t mask[2];
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
                 const int m = mt * 16 + n + 8 * o;
                 const bool there = m < n_rows;
                 const int r = there ? r0 + m / G : 0;
-                row_r[mt][o] = there ? r : -1;
                 const __nv_bfloat16* q = bp.q + (((size_t)s.b * R + r) * Hq + s.g * G + (there ? m % G : 0)) * D;
                 float amax = 0.f;
 #pragma unroll
@@ -158,17 +175,20 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
                     const uint2 v = there ? __ldg(reinterpret_cast<const uint2*>(q + piece * 16 + (j % 4) * 4)) : make_uint2(0u, 0u);
                     raw[o][j][0] = v.x;
                     raw[o][j][1] = v.y;
+                }
+                mask[o] = there ? pv.mask[(size_t)s.b * kMaxRows + r] : 0ull;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         amax = fmaxf(amax, fabsf(__uint_as_float(raw[o][j][k] << 16)));
                         amax = fmaxf(amax, fabsf(__uint_as_float(raw[o][j][k] & 0xffff0000u)));
                     }
-                }
                 amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
                 amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
                 // 2^e <= amax < 2^(e + 1); both it and its reciprocal are normal numbers
                 const int e = min(max((int)(__float_as_uint(amax) >> 23) - 127, -125), 125);
-                q_scale[mt][o] = prm.c * __uint_as_float((uint32_t)(e + 127) << 23);
+                scale[o] = prm.c * __uint_as_float((uint32_t)(e + 127) << 23);
                 const float down = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j)
@@ -176,46 +196,73 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
                     for (int k = 0; k < 2; ++k)
                         raw[o][j][k] = pack_f16(__uint_as_float(raw[o][j][k] << 16) * down, __uint_as_float(raw[o][j][k] & 0xffff0000u) * down);
             }
-            if (warp == 0)
+            // (it is all here by the time that the warps are done with the run before's)
+            if (mt == 0 && !__all_sync(0xffffffffu, mbar_wait(&sh.q_empty, (seg & 1) ^ 1, &sh.abort, prm.wait_ns))) return;
+            if (x == 0)
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) sh.q[mt][j][lane] = make_uint4(raw[0][j][0], raw[1][j][0], raw[0][j][1], raw[1][j][1]);
+                for (int o = 0; o < 2; ++o) {
+                    sh.q_scale[mt * 16 + n + 8 * o] = scale[o];
+                    sh.mask[mt * 16 + n + 8 * o] = mask[o];
+                }
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) sh.q[mt][j][lane] = make_uint4(raw[0][j][0], raw[1][j][0], raw[0][j][1], raw[1][j][1]);
         }
-        sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_full);
+    }
+}
 
-        float m_ref[kMt][2], l[kMt][2], o_acc[kMt][D / 8][4];
+template <int D, typename Sh>
+__device__ void consumer_role(Sh& sh, const Params& prm, const PlanView& pv)
+{
+    constexpr int kMt = Sh::kMt;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n = lane >> 2, x = lane & 3;
+    const int G = prm.G, T = prm.d.T, R = prm.d.T + prm.d.C, S = prm.d.S, Hq = prm.d.Hq;
+    // bytes of a lane's pieces in a chunk.  K: key row 8 t + n, pieces 2 x and 2 x + 1 (D = 64: piece x); V: key rows 8 t + 2 x + o, the D / 8 bytes
+    // from n * D / 8 on.
+    uint32_t k_at[D / 64], v_at[2];
+    if constexpr (D == 128) {
+        k_at[0] = (uint32_t)(n * 128 + (((2 * x) ^ n) << 4));
+        k_at[D / 64 - 1] = (uint32_t)(n * 128 + (((2 * x + 1) ^ n) << 4));
+    } else
+        k_at[0] = (uint32_t)(n * 64 + ((x ^ (n >> 1)) << 4));
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+        v_at[o] = D == 128 ? (uint32_t)((2 * x + o) * 128 + ((n ^ (2 * x + o)) << 4)) : (uint32_t)((2 * x + o) * 64 + (((n >> 1) ^ x) << 4) + (n & 1) * 8);
+    auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(Sh::kWarps * 32) : "memory"); };
+
+    Walker w;
+    Segment s, ahead;
+    bool ok = true;
+    uint32_t i0 = 0, seg = 0, n_met = 0;             // chunks and runs before this one; times that the warps have met
+    bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s);
+    for (; run; ++seg) {
+        const bool more = w.next(ahead);             // (read now: it is there when this run ends)
+        const int r0 = prm.rpt * prm.tpg * s.rg, n_rows = min(R - r0, prm.rpt * prm.tpg) * G;
+        const int keys = (int)s.P + R;
+        const Chunks ch(s, keys, S);
+        ok = __all_sync(0xffffffffu, mbar_wait(&sh.q_full, seg & 1, &sh.abort, prm.wait_ns)) && ok;
+        float q_scale[kMt][2], m_ref[kMt][2], l[kMt][2], o_acc[kMt][D / 8][4];       // of the lane's rows n and n + 8 of an M tile
 #pragma unroll
         for (int mt = 0; mt < kMt; ++mt) {
             m_ref[mt][0] = m_ref[mt][1] = -INFINITY;
             l[mt][0] = l[mt][1] = 0.f;
+            q_scale[mt][0] = sh.q_scale[mt * 16 + n];
+            q_scale[mt][1] = sh.q_scale[mt * 16 + n + 8];
 #pragma unroll
             for (int u = 0; u < D / 8; ++u) o_acc[mt][u][0] = o_acc[mt][u][1] = o_acc[mt][u][2] = o_acc[mt][u][3] = 0.f;
         }
 
-        // ---- the keys: tile number i of the walk is group i % kGroups's, in stage i % kStages ----
-        const int32_t* table = prm.map.block_table + (size_t)s.b * prm.map.max_pages;
-        int page_base = s.t0 - 32, pages = -1;       // a lane's page of 32 tiles
-        auto scales_of = [&](int t) -> float2 {
-            if (t >= s.t1) return make_float2(1.f, 1.f);
-            if (t - page_base >= 32) {
-                page_base = t;
-                pages = t + lane < min(s.t1, s.nkt) ? __ldg(table + t + lane) : -1;
-            }
-            const int page = __shfl_sync(0xffffffffu, pages, t - page_base);
-            const bool soft = t >= s.nkt;
-            const bool there = soft ? sub * kChunk < S : (uint32_t)page < (uint64_t)bp.n_pages && (int64_t)t * kTileKeys + sub * kChunk < s.P + R;
-            const size_t at = ((size_t)(soft || !there ? 0 : page) * Hkv + s.g) * nb + sub_block;
-            return there ? make_float2(__ldg((soft ? bp.ks_soft : bp.ks) + at), __ldg((soft ? bp.vs_soft : bp.vs) + at)) : make_float2(1.f, 1.f);
-        };
-        int t = s.t0 + (int)((uint32_t)(group + kGroups - i0 % kGroups) % kGroups);
-        float2 scale = scales_of(t);
+        // ---- the keys: this warp's chunks of the run ----
 #pragma unroll 1
-        for (; t < s.t1; t += kGroups) {
-            const float2 scale_next = scales_of(t + kGroups);
-            const uint32_t i = i0 + (uint32_t)(t - s.t0), st = i % Sh::kStages;
-            const int64_t left = t >= s.nkt ? S - sub * kChunk : s.P + R - ((int64_t)t * kTileKeys + sub * kChunk);
-            ok = __all_sync(0xffffffffu, mbar_wait(&sh.full[st], (i / Sh::kStages) & 1, &sh.abort, prm.wait_ns)) && ok;
-            if (left > 0 && ok) {
-                const uint8_t *k_tile = sh.kv[st][0], *v_tile = sh.kv[st][1];
+        for (int j = (warp + Sh::kWarps - (int)(i0 % Sh::kWarps)) % Sh::kWarps; j < ch.n; j += Sh::kWarps) {
+            const Place<Sh> at(i0 + (uint32_t)j);
+            const int t = ch.tile(s, j), sub = ch.sub(j), left = (t >= s.nkt ? S : keys - t * kTileKeys) - sub * kChunk;
+            ok = __all_sync(0xffffffffu, mbar_wait(&sh.full[warp][at.slot], at.parity, &sh.abort, prm.wait_ns)) && ok;
+            if (ok) {
+                const uint8_t *k_tile = sh.kv[warp][at.slot][0], *v_tile = sh.kv[warp][at.slot][1];
+                const float4 scale = sh.scales[warp][at.slot];
                 // ---- scores ----
                 float sc[kMt][4][4];
 #pragma unroll
@@ -228,21 +275,20 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
 #pragma unroll
                     for (int u = 0; u < 4; ++u) kw[u] = *reinterpret_cast<const uint4*>(k_tile + k_at[h] + 8 * u * D);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int jj = 0; jj < 4; ++jj) {
                         uint4 a[kMt];
 #pragma unroll
-                        for (int mt = 0; mt < kMt; ++mt) a[mt] = sh.q[mt][4 * h + j][lane];
+                        for (int mt = 0; mt < kMt; ++mt) a[mt] = sh.q[mt][4 * h + jj][lane];
 #pragma unroll
                         for (int u = 0; u < 4; ++u) {
                             uint32_t b0, b1;
-                            e4m3_to_f16x4(j == 0 ? kw[u].x : j == 1 ? kw[u].y : j == 2 ? kw[u].z : kw[u].w, b0, b1);
+                            e4m3_to_f16x4(jj == 0 ? kw[u].x : jj == 1 ? kw[u].y : jj == 2 ? kw[u].z : kw[u].w, b0, b1);
 #pragma unroll
                             for (int mt = 0; mt < kMt; ++mt) mma_f16(sc[mt][u], a[mt], b0, b1);
                         }
                     }
                 }
                 // ---- weights ----
-                const float vs = fmaxf(scale.y, kLeastScale), off = log2f(vs), inv_vs = 1.f / vs;
                 uint4 p[kMt][2];                     // A fragments of 16 keys: key tiles 2 h and 2 h + 1
 #pragma unroll
                 for (int mt = 0; mt < kMt; ++mt) {
@@ -250,15 +296,15 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
 #pragma unroll
                         for (int o = 0; o < 2; ++o) {
                             uint64_t lo, hi;
-                            const int r = row_r[mt][o];
-                            visible_bits(s, t, R, T, S, r, r >= 0, r >= 0 ? pv.mask[(size_t)s.b * kMaxRows + r] : 0ull, lo, hi);
+                            const int m = mt * 16 + n + 8 * o;
+                            visible_bits(s, t, R, T, S, r0 + m / G, m < n_rows, sh.mask[m], lo, hi);
                             const uint32_t vis = (uint32_t)((sub & 2 ? hi : lo) >> (32 * (sub & 1)));
 #pragma unroll
                             for (int u = 0; u < 4; ++u)
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
                                     if (!((vis >> (8 * u + 2 * x + k)) & 1u)) sc[mt][u][2 * o + k] = -INFINITY;
-                                    if (r < 0) sc[mt][u][2 * o + k] = 0.f;       // (a row that does not exist)
+                                    if (m >= n_rows) sc[mt][u][2 * o + k] = 0.f;       // (a row that does not exist)
                                 }
                         }
                     }
@@ -272,12 +318,12 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         // (a factor of 0 would turn the -infinity of masked keys into NaN)
                         a_row[o] = fmaxf(q_scale[mt][o] * scale.x, 1.1754944e-38f);
-                        const float m_new = fmaxf(m_ref[mt][o], fmaf(top, a_row[o], off));
+                        const float m_new = fmaxf(m_ref[mt][o], fmaf(top, a_row[o], scale.y));
                         const bool mv = m_new - m_ref[mt][o] > kRescaleThreshold;        // false when both are -inf (NaN)
                         alpha[o] = mv ? ex2(m_ref[mt][o] - m_new) : 1.f;
                         if (mv) m_ref[mt][o] = m_new;
                         move = move || mv;
-                        add[o] = off - (m_ref[mt][o] == -INFINITY ? 0.f : m_ref[mt][o]);
+                        add[o] = scale.y - (m_ref[mt][o] == -INFINITY ? 0.f : m_ref[mt][o]);
                     }
                     if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
@@ -300,7 +346,7 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
                             sum += x0 + x1;
                             pk[o][u] = pack_f16(x0, x1);
                         }
-                        l[mt][o] = fmaf(sum, inv_vs, l[mt][o]);
+                        l[mt][o] = fmaf(sum, scale.z, l[mt][o]);
                     }
                     p[mt][0] = make_uint4(pk[0][0], pk[1][0], pk[0][1], pk[1][1]);
                     p[mt][1] = make_uint4(pk[0][2], pk[1][2], pk[0][3], pk[1][3]);
@@ -313,18 +359,23 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
                     for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int o = 0; o < 2; ++o) {
-                            const uint8_t* at = v_tile + v_at[o] + 8 * (2 * h + u) * D;
+                            const uint8_t* from = v_tile + v_at[o] + 8 * (2 * h + u) * D;
                             if constexpr (D == 128) {
-                                const uint4 v = *reinterpret_cast<const uint4*>(at);
+                                const uint4 v = *reinterpret_cast<const uint4*>(from);
                                 vw[u][o][0] = v.x; vw[u][o][1] = v.y; vw[u][o][2] = v.z; vw[u][o][3] = v.w;
                             } else {
-                                const uint2 v = *reinterpret_cast<const uint2*>(at);
+                                const uint2 v = *reinterpret_cast<const uint2*>(from);
                                 vw[u][o][0] = v.x; vw[u][o][1] = v.y;
                             }
-                            if (left < kChunk && 8 * (2 * h + u) + 2 * x + o >= (int)left)
-#pragma unroll
-                                for (int k = 0; k < D / 32; ++k) vw[u][o][k] = 0u;
                         }
+                    if (left < kChunk)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int o = 0; o < 2; ++o)
+                                if (8 * (2 * h + u) + 2 * x + o >= left)
+#pragma unroll
+                                    for (int k = 0; k < D / 32; ++k) vw[u][o][k] = 0u;
 #pragma unroll
                     for (int k = 0; k < D / 32; ++k) {       // four columns of a lane
                         uint32_t b0[4], b1[4];
@@ -340,101 +391,101 @@ __device__ void consumer_role(SharedStorage<D, kMt, kGroups>& sh, const Params& 
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.empty[st]);
-            scale = scale_next;
+            if (lane == 0) mbar_arrive(&sh.empty[warp][at.slot]);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_empty);
 
-        // ---- the end of a run: the warps meet ----
+        // ---- the end of a run: the warps meet, 4 or 16 rows at a time ----
+        constexpr int kVec = D / 4;                  // float4s of a row
+        const bool whole = s.part_slot < 0;
 #pragma unroll
         for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
                 l[mt][o] += __shfl_xor_sync(0xffffffffu, l[mt][o], 1);
                 l[mt][o] += __shfl_xor_sync(0xffffffffu, l[mt][o], 2);
-                if (x == 0) sh.stat[warp][mt * 16 + n + 8 * o] = make_float2(m_ref[mt][o], l[mt][o]);
             }
-        sync();
-        // own sums at the rows' maximum, added to those of the same quarter's warps in the groups before
-#pragma unroll 1
-        for (int k = 0; k < kGroups; ++k) {
-            if (group == k)
 #pragma unroll
-                for (int mt = 0; mt < kMt; ++mt)
+        for (int pass = 0; pass < kMt * 16 / Sh::kRowsAtOnce; ++pass) {
+            const int row0 = pass * Sh::kRowsAtOnce;
+            if (row0 >= n_rows) break;
+            // (what the warps wrote the last time they met has been read by all of them)
+            if (n_met > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sh.met, (n_met - 1) & 1, &sh.abort, prm.wait_ns)) && ok;
 #pragma unroll
-                    for (int o = 0; o < 2; ++o) {
-                        const int row = mt * 16 + n + 8 * o;
-                        if (row >= n_rows) continue;
-                        float M = -INFINITY;
+            for (int q = 0; q < kMt; ++q) {
+                // one M tile: rows 4 pass .. 4 pass + 3, of the lanes with n / 4 = pass % 2; two: the 16 rows of M tile `pass`
+                const int mt = kMt == 1 ? 0 : pass, o = kMt == 1 ? pass / 2 : q;
+                const int row = kMt == 1 ? n & 3 : n + 8 * q;                 // of this pass
+                if (row0 + row < n_rows && (kMt == 2 || n / 4 == pass % 2)) {
+                    if (x == 0) sh.stat[warp][row] = make_float2(m_ref[mt][o], l[mt][o]);
+                    // columns n' of a product's tile u: head dim n' * D / 8 + u; the lane's two columns are 2 x and 2 x + 1: D / 4 contiguous head dims
+                    float* to = &sh.sums[warp][row][x * Sh::kSeg];
 #pragma unroll
-                        for (int v = 0; v < Sh::kWarps; ++v) M = fmaxf(M, sh.stat[v][row].x);
-                        const float f = m_ref[mt][o] == -INFINITY ? 0.f : ex2(m_ref[mt][o] - M);
-                        // columns n' of a product's tile u: head dim n' * D / 8 + u; the lane's two columns are 2 x and 2 x + 1: D / 4 contiguous head dims
-                        float* to = &sh.sums[sub][row][x * Sh::kSeg];
-#pragma unroll
-                        for (int u = 0; u < D / 4; u += 4) {
-                            const int c = u < D / 8 ? 2 * o : 2 * o + 1, v = u % (D / 8);
-                            float4 acc = k == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(to + u);
-                            acc.x = fmaf(f, o_acc[mt][v][c], acc.x);
-                            acc.y = fmaf(f, o_acc[mt][v + 1][c], acc.y);
-                            acc.z = fmaf(f, o_acc[mt][v + 2][c], acc.z);
-                            acc.w = fmaf(f, o_acc[mt][v + 3][c], acc.w);
-                            *reinterpret_cast<float4*>(to + u) = acc;
-                        }
+                    for (int u = 0; u < D / 4; u += 4) {
+                        const int c = u < D / 8 ? 2 * o : 2 * o + 1, v = u % (D / 8);
+                        *reinterpret_cast<float4*>(to + u) = make_float4(o_acc[mt][v][c], o_acc[mt][v + 1][c], o_acc[mt][v + 2][c], o_acc[mt][v + 3][c]);
                     }
-            sync();
-        }
-        constexpr int kVec = D / 4;                  // float4s of a row
-        const bool whole = s.part_slot < 0;
-        for (int i = threadIdx.x; i < n_rows * kVec; i += Sh::kWarps * 32) {
-            const int m = i / kVec, v = i % kVec;
-            float M = -INFINITY, L = 0.f;
-#pragma unroll
-            for (int k = 0; k < Sh::kWarps; ++k) M = fmaxf(M, sh.stat[k][m].x);
-#pragma unroll
-            for (int k = 0; k < Sh::kWarps; ++k) {
-                const float2 ml = sh.stat[k][m];
-                L = fmaf(ml.x == -INFINITY ? 0.f : ex2(ml.x - M), ml.y, L);
-            }
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float4 y = *reinterpret_cast<const float4*>(&sh.sums[k][m][(v / (kVec / 4)) * Sh::kSeg + (v % (kVec / 4)) * 4]);
-                acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
-            }
-            const int r = r0 + m / G;
-            if (whole) {
-                const size_t row_out = ((size_t)s.b * R + r) * Hq + s.g * G + m % G;
-                const float inv = 1.f / L;
-                reinterpret_cast<uint2*>(prm.out + row_out * D)[v] = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                if (prm.lse && v == 0) prm.lse[row_out] = natural_lse(M, L);
-            } else {
-                float* part = prm.partials + (size_t)s.part_slot * (partial_slot_bytes() / sizeof(float));
-                const int mt = (r - r0) / prm.rpt, at = mt * 128 + (r - r0 - mt * prm.rpt) * G + m % G;
-                reinterpret_cast<float4*>(part + (size_t)at * kPartD)[v] = acc;
-                if (v == 0) {
-                    part[(size_t)kPartRows * kPartD + at] = M;
-                    part[(size_t)kPartRows * kPartD + kPartRows + at] = L;
                 }
             }
+            sync();
+            const int here = min(n_rows - row0, Sh::kRowsAtOnce);
+            for (int e = threadIdx.x; e < here * kVec; e += Sh::kWarps * 32) {
+                const int row = e / kVec, v = e % kVec, m = row0 + row;
+                float M = -INFINITY, L = 0.f;
+#pragma unroll
+                for (int k = 0; k < Sh::kWarps; ++k) M = fmaxf(M, sh.stat[k][row].x);
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int k = 0; k < Sh::kWarps; ++k) {
+                    const float2 ml = sh.stat[k][row];
+                    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+                    const float4 y = *reinterpret_cast<const float4*>(&sh.sums[k][row][(v / (kVec / 4)) * Sh::kSeg + (v % (kVec / 4)) * 4]);
+                    L = fmaf(f, ml.y, L);
+                    acc.x = fmaf(f, y.x, acc.x);
+                    acc.y = fmaf(f, y.y, acc.y);
+                    acc.z = fmaf(f, y.z, acc.z);
+                    acc.w = fmaf(f, y.w, acc.w);
+                }
+                const int r = r0 + m / G;
+                if (whole) {
+                    const size_t row_out = ((size_t)s.b * R + r) * Hq + s.g * G + m % G;
+                    const float inv = 1.f / L;
+                    reinterpret_cast<uint2*>(prm.out + row_out * D)[v] = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                    if (prm.lse && v == 0) prm.lse[row_out] = natural_lse(M, L);
+                } else {
+                    float* part = prm.partials + (size_t)s.part_slot * (partial_slot_bytes() / sizeof(float));
+                    const int mt = (r - r0) / prm.rpt, at = mt * 128 + (r - r0 - mt * prm.rpt) * G + m % G;
+                    reinterpret_cast<float4*>(part + (size_t)at * kPartD)[v] = acc;
+                    if (v == 0) {
+                        part[(size_t)kPartRows * kPartD + at] = M;
+                        part[(size_t)kPartRows * kPartD + kPartRows + at] = L;
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.met);
+            ++n_met;
         }
-        // (the next run's Q goes into shared memory before its first barrier, but nobody reads it here; its statistics and sums come
-        // behind that barrier)
-        i0 += (uint32_t)(s.t1 - s.t0);
+        i0 += (uint32_t)ch.n;
         s = ahead;
         run = more;
     }
 }
 
-template <int D, int kMt, int kGroups>
-__global__ void __launch_bounds__(SharedStorage<D, kMt, kGroups>::kThreads, 1)
+template <int D, int kMt, int kWarps>
+__global__ void __launch_bounds__(SharedStorage<D, kMt, kWarps>::kThreads, 1)
 attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap ks_map,
                        const __grid_constant__ CUtensorMap vs_map, const Params prm, const BlockParams bp)
 {
-    using Sh = SharedStorage<D, kMt, kGroups>;
+    using Sh = SharedStorage<D, kMt, kWarps>;
     extern __shared__ uint8_t smem_raw[];
     Sh& sh = *reinterpret_cast<Sh*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 4); }
+        for (int i = 0; i < Sh::kWarps * Sh::kSlots; ++i) { mbar_init(&sh.full[0][0] + i, 1); mbar_init(&sh.empty[0][0] + i, 1); }
+        mbar_init(&sh.q_full, 1);
+        mbar_init(&sh.q_empty, Sh::kWarps);
+        mbar_init(&sh.met, Sh::kWarps);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -445,11 +496,13 @@ attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     // registers: 512 x 128 = 384 x 152 + 128 x 56, or 384 x 168 = 256 x 224 + 128 x 56
     if (threadIdx.x >= Sh::kWarps * 32) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (threadIdx.x < Sh::kWarps * 32 + 32) producer_role(sh, prm, bp, pv, &k_map, &v_map, &ks_map, &vs_map);
+        const int role = (threadIdx.x >> 5) - Sh::kWarps;
+        if (role == 0) fetch_role<D>(sh, prm, bp, pv, &k_map, &v_map, &ks_map, &vs_map);
+        else if (role == 1) q_role<D>(sh, prm, bp, pv);
         __syncwarp();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kGroups == 3 ? 152 : 224));
-        consumer_role(sh, prm, bp, pv);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWarps == 12 ? 152 : 224));
+        consumer_role<D>(sh, prm, pv);
     }
     __syncthreads();
     if (sh.abort) {
@@ -461,14 +514,14 @@ attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     }
 }
 
-template <int D, int kMt, int kGroups>
+template <int D, int kMt, int kWarps>
 cudaError_t launch(const CUtensorMap (&maps)[4], const Params& prm, const BlockParams& bp, int units, cudaStream_t st)
 {
-    using Sh = SharedStorage<D, kMt, kGroups>;
+    using Sh = SharedStorage<D, kMt, kWarps>;
     constexpr int smem = (int)sizeof(Sh) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory of a CTA");
     static OncePerDevice attr_done;
-    cudaError_t e = attr_done.run([&] { return cudaFuncSetAttribute(attention_block_kernel<D, kMt, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
+    cudaError_t e = attr_done.run([&] { return cudaFuncSetAttribute(attention_block_kernel<D, kMt, kWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute pdl[1];
     pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -480,7 +533,7 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const Params& prm, const BlockP
     cfg.stream = st;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_block_kernel<D, kMt, kGroups>, maps[0], maps[1], maps[2], maps[3], prm, bp);
+    return cudaLaunchKernelEx(&cfg, attention_block_kernel<D, kMt, kWarps>, maps[0], maps[1], maps[2], maps[3], prm, bp);
 }
 
 }  // namespace blk
@@ -495,8 +548,8 @@ cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const vo
 {
     using namespace tc;
     CUtensorMap maps[4];
-    bool ok = make_code_map(&maps[0], k_cache, n_slots, d.Hkv, d.D) && make_code_map(&maps[1], v_cache, n_slots, d.Hkv, d.D);
-    if (d.S > 0) ok = ok && make_code_map(&maps[2], k_soft, d.S, d.Hkv, d.D) && make_code_map(&maps[3], v_soft, d.S, d.Hkv, d.D);
+    bool ok = make_code_map(&maps[0], k_cache, n_slots, d.Hkv, blk::kChunk, d.D) && make_code_map(&maps[1], v_cache, n_slots, d.Hkv, blk::kChunk, d.D);
+    if (d.S > 0) ok = ok && make_code_map(&maps[2], k_soft, d.S, d.Hkv, blk::kChunk, d.D) && make_code_map(&maps[3], v_soft, d.S, d.Hkv, blk::kChunk, d.D);
     else { maps[2] = maps[0]; maps[3] = maps[1]; }
     if (!ok) return cudaErrorInvalidValue;
     Params prm;
@@ -523,8 +576,8 @@ cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const vo
     bp.block = ctx->block;
     const int units = ctx->sm_count;
     cudaError_t e;
-    if ((d.T + d.C) * prm.G <= 16) e = d.D == 64 ? blk::launch<64, 1, 3>(maps, prm, bp, units, st) : blk::launch<128, 1, 3>(maps, prm, bp, units, st);
-    else e = d.D == 64 ? blk::launch<64, 2, 2>(maps, prm, bp, units, st) : blk::launch<128, 2, 2>(maps, prm, bp, units, st);
+    if ((d.T + d.C) * prm.G <= 16) e = d.D == 64 ? blk::launch<64, 1, 12>(maps, prm, bp, units, st) : blk::launch<128, 1, 12>(maps, prm, bp, units, st);
+    else e = d.D == 64 ? blk::launch<64, 2, 8>(maps, prm, bp, units, st) : blk::launch<128, 2, 8>(maps, prm, bp, units, st);
     if (e != cudaSuccess) return e;
     return launch_combine(prm, ctx->sm_count, st);
 }

@@ -20,7 +20,7 @@ namespace confu {
 namespace tc {
 
 bool make_tile_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t box_rows, uint32_t box_heads, uint32_t head_dim);
-bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t head_dim);
+bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t box_rows, uint32_t head_dim);
 
 namespace blktc {
 
@@ -660,8 +660,8 @@ cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const
     bp.n_pages = n_slots / kTileKeys;
     bp.block = ctx->block;
     CUtensorMap maps[3];
-    if (!make_tile_map(&maps[0], q, (uint64_t)d.B * (d.T + d.C), d.Hq, prm.rpt, prm.G, d.D) || !make_code_map(&maps[1], k_cache, n_slots, d.Hkv, d.D) ||
-        !make_code_map(&maps[2], v_cache, n_slots, d.Hkv, d.D))
+    if (!make_tile_map(&maps[0], q, (uint64_t)d.B * (d.T + d.C), d.Hq, prm.rpt, prm.G, d.D) || !make_code_map(&maps[1], k_cache, n_slots, d.Hkv, kTileKeys, d.D) ||
+        !make_code_map(&maps[2], v_cache, n_slots, d.Hkv, kTileKeys, d.D))
         return cudaErrorInvalidValue;
     const cudaError_t e = d.D == 64 ? blktc::launch<64>(maps, prm, bp, ctx->sm_count, st) : blktc::launch<128>(maps, prm, bp, ctx->sm_count, st);
     if (e != cudaSuccess) return e;

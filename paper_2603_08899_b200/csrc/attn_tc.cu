@@ -539,15 +539,15 @@ bool make_tile_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t h
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// [rows][heads][head_dim] tensor of bytes, box = 128 rows x 1 head x head_dim bytes; rows of the box are swizzled by their own
+// [rows][heads][head_dim] tensor of bytes, box = box_rows x 1 head x head_dim bytes; rows of the box are swizzled by their own
 // length (128 or 64 bytes).  (Rows of one head lie a head's row apart from the next head's: wider L2 fetches would read the neighbour too.)
-bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t head_dim)
+bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint32_t box_rows, uint32_t head_dim)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)head_dim, heads, rows};
     const cuuint64_t strides[2] = {(cuuint64_t)head_dim, heads * head_dim};
-    const cuuint32_t box[3] = {head_dim, 1, (cuuint32_t)kTileKeys};
+    const cuuint32_t box[3] = {head_dim, 1, box_rows};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
