@@ -10,7 +10,7 @@
 //
 // Up to 32 rows (query rows x heads of a kv head): reading the cache binds, 2 D bytes a key, and what counts is how many
 // bytes are on their way.  One CTA per SM walks its share of key tiles in chunks of 32 keys, which 12 warps (8 for more than 16 rows) take in turn.
-// Every warp has a ring of two chunks of its own (K and V codes, 8 KB at D = 128); the lanes of one warp keep them filled by TMA, across the ends of
+// Every warp has a ring of two chunks of its own (K and V codes, 8 KB at D = 128); lanes of three warps keep them filled by TMA, across the ends of
 // runs, another warp lays out the next run's Q.  (Codes loaded straight into the registers that the products read, 8 KB a warp
 // under way: 64 sequences of 100..8192, one row, 203 us a layer at 2.8 TB/s, the warps waiting for their loads half of the time.)
 //   S = Q K^T    a lane's fragment of K^T is 16 contiguous bytes of a key (the head dims of a product's 16 steps are whatever
@@ -64,6 +64,27 @@ struct SharedStorage {
     int abort;
 };
 
+// The CTA's runs.  By heads a run's row group stands for the kv head (few rows: there is one group).
+__device__ __forceinline__ void by_head(const Params& prm, Segment& s)
+{
+    if (prm.kind == kPlanHeads) {
+        s.g = s.rg;
+        s.rg = 0;
+    }
+}
+__device__ __forceinline__ bool begin_walk(Walker& w, const PlanView& pv, const Params& prm, Segment& s)
+{
+    const bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s);
+    by_head(prm, s);
+    return run;
+}
+__device__ __forceinline__ bool next_run(Walker& w, const Params& prm, Segment& s)
+{
+    const bool run = w.next(s);
+    if (run) by_head(prm, s);
+    return run;
+}
+
 // The chunks of a run that hold keys: those of its key tiles up to the last slot, then those of the soft prompts.
 struct Chunks {
     int n_keys, n;
@@ -99,18 +120,18 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 }
 
 // Fills the rings, a lane for each: K and V of the warp's chunks of the share, one after the other, and their scales.  The page of a chunk is looked up
-// two chunks ahead, its scales one.  (One lane for all rings, in order: 64 sequences of 100..8192 165 us a layer, 136 without any arithmetic on
-// the keys; the loop of that lane was what bound.)
+// two chunks ahead, its scales one.  Lanes of a warp issue their copies one after the other, so three warps share the rings.  (One lane for all rings, in
+// order: 64 sequences of 100..8192 165 us a layer, 136 without any arithmetic on the keys: that loop was what bound; a lane per ring in one warp
+// 122, in three 108.)
 template <int D, typename Sh>
-__device__ void fetch_role(Sh& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, const CUtensorMap* k_map, const CUtensorMap* v_map,
+__device__ void fetch_role(Sh& sh, int ring, const Params& prm, const BlockParams& bp, const PlanView& pv, const CUtensorMap* k_map, const CUtensorMap* v_map,
                            const CUtensorMap* ks_map, const CUtensorMap* vs_map)
 {
-    const int ring = threadIdx.x & 31, nb = kTileKeys / bp.block;
-    if (ring >= Sh::kWarps) return;
+    const int nb = kTileKeys / bp.block;
     Walker w;
     Segment s;
     uint32_t i0 = 0;
-    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s)) {
+    for (bool run = begin_walk(w, pv, prm, s); run; run = next_run(w, prm, s)) {
         const Chunks ch(s, (int)s.P + prm.d.T + prm.d.C, prm.d.S);
         const int32_t* table = prm.map.block_table + (size_t)s.b * prm.map.max_pages;
         // (soft prompts have scales like a page's; -1: outside the pool, or no such chunk)
@@ -130,20 +151,37 @@ __device__ void fetch_role(Sh& sh, const Params& prm, const BlockParams& bp, con
             const Place<Sh> at(i0 + (uint32_t)j);
             if (!mbar_wait(&sh.empty[ring][at.slot], at.parity ^ 1, &sh.abort, prm.wait_ns)) return;
             const bool soft = j >= ch.n_keys;
-            const float vs = fmaxf(scale.y, kLeastScale);
-            sh.scales[ring][at.slot] = make_float4(scale.x, log2f(vs), 1.f / vs, 0.f);
             // (outside the pool: a box that lies before it reads as zeros)
             const int z = soft ? ch.sub(j) * kChunk : (uint32_t)page < (uint64_t)bp.n_pages ? page * kTileKeys + (j & 3) * kChunk : -kTileKeys;
             uint64_t* full = &sh.full[ring][at.slot];
             mbar_arrive_expect_tx(full, 2 * Sh::kCodes);
             tma_load_3d(sh.kv[ring][at.slot][0], soft ? ks_map : k_map, full, 0, s.g, z);
             tma_load_3d(sh.kv[ring][at.slot][1], soft ? vs_map : v_map, full, 0, s.g, z);
+            // (the scales may be here later than the page)
+            const float vs = fmaxf(scale.y, kLeastScale);
+            sh.scales[ring][at.slot] = make_float4(scale.x, log2f(vs), 1.f / vs, 0.f);
+            mbar_arrive(full);
             page = page_next;
             page_next = page_after;
             scale = scale_next;
         }
         i0 += (uint32_t)ch.n;
     }
+}
+
+// A ring's first chunk into L2 while the kernels before this one still run: a hint, as in tc_walk.cuh.  The plan may not be there yet, K and V
+// may still be written; nothing that is read here is used for anything else.
+template <int D, typename Sh>
+__device__ __forceinline__ void fetch_ahead(int ring, const Params& prm, const BlockParams& bp, const PlanView& pv, const CUtensorMap* k_map, const CUtensorMap* v_map)
+{
+    const int4* w = reinterpret_cast<const int4*>(pv.cta + blockIdx.x);
+    const int4 w0 = __ldcg(w), w1 = __ldcg(w + 1);
+    const int b = w0.x, g = prm.kind == kPlanHeads ? w0.y >> 16 : w0.y & 0xffff, t = w0.z + (ring >> 2);
+    if (b < 0 || b >= prm.d.B || g < 0 || g >= prm.d.Hkv || w0.z < 0 || t >= w0.w || t >= w1.x - (prm.d.S > 0 ? 1 : 0) || t >= prm.map.max_pages) return;
+    const int page = __ldcg(prm.map.block_table + (size_t)b * prm.map.max_pages + t);
+    if ((uint32_t)page >= (uint64_t)bp.n_pages) return;
+    tma_prefetch_3d(k_map, 0, g, page * kTileKeys + (ring & 3) * kChunk);
+    tma_prefetch_3d(v_map, 0, g, page * kTileKeys + (ring & 3) * kChunk);
 }
 
 // Q of a run, while the run before it is walked: rows of the group, head by head; row m of it is query row r0 + m / G, head m % G of the kv head's.
@@ -155,7 +193,7 @@ __device__ void q_role(Sh& sh, const Params& prm, const BlockParams& bp, const P
     Walker w;
     Segment s;
     uint32_t seg = 0;
-    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s), ++seg) {
+    for (bool run = begin_walk(w, pv, prm, s); run; run = next_run(w, prm, s), ++seg) {
         const int r0 = prm.rpt * prm.tpg * s.rg, n_rows = min(R - r0, prm.rpt * prm.tpg) * G;
 #pragma unroll 1
         for (int mt = 0; mt < Sh::kMt; ++mt) {
@@ -233,12 +271,12 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const PlanView& pv)
     auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(Sh::kWarps * 32) : "memory"); };
 
     Walker w;
-    Segment s, ahead;
+    Segment s;
     bool ok = true;
     uint32_t i0 = 0, seg = 0, n_met = 0;             // chunks and runs before this one; times that the warps have met
-    bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s);
+    bool run = begin_walk(w, pv, prm, s);
     for (; run; ++seg) {
-        const bool more = w.next(ahead);             // (read now: it is there when this run ends)
+        if (w.left > 1) asm volatile("prefetch.global.L1 [%0];" ::"l"(w.cur + 1));        // (the next run: it is there when this one ends)
         const int r0 = prm.rpt * prm.tpg * s.rg, n_rows = min(R - r0, prm.rpt * prm.tpg) * G;
         const int keys = (int)s.P + R;
         const Chunks ch(s, keys, S);
@@ -468,8 +506,7 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const PlanView& pv)
             ++n_met;
         }
         i0 += (uint32_t)ch.n;
-        s = ahead;
-        run = more;
+        run = next_run(w, prm, s);
     }
 }
 
@@ -482,7 +519,8 @@ attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     extern __shared__ uint8_t smem_raw[];
     Sh& sh = *reinterpret_cast<Sh*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < Sh::kWarps * Sh::kSlots; ++i) { mbar_init(&sh.full[0][0] + i, 1); mbar_init(&sh.empty[0][0] + i, 1); }
+        // full: the copies (announced by one arrival) and the scales
+        for (int i = 0; i < Sh::kWarps * Sh::kSlots; ++i) { mbar_init(&sh.full[0][0] + i, 2); mbar_init(&sh.empty[0][0] + i, 1); }
         mbar_init(&sh.q_full, 1);
         mbar_init(&sh.q_empty, Sh::kWarps);
         mbar_init(&sh.met, Sh::kWarps);
@@ -492,13 +530,16 @@ attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     }
     __syncthreads();
     const PlanView pv = plan_view(const_cast<void*>(prm.plan), prm.d.B, prm.d.Hkv);
+    constexpr int kPer = (kWarps + 2) / 3;           // rings of a fetching warp
+    const int role = (threadIdx.x >> 5) - Sh::kWarps, lane = threadIdx.x & 31, ring = lane < kPer && role < 3 && role * kPer + lane < kWarps ? role * kPer + lane : -1;
+    if (prm.prefetch && role >= 0 && ring >= 0) fetch_ahead<D, Sh>(ring, prm, bp, pv, &k_map, &v_map);
+    __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // registers: 512 x 128 = 384 x 152 + 128 x 56, or 384 x 168 = 256 x 224 + 128 x 56
     if (threadIdx.x >= Sh::kWarps * 32) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        const int role = (threadIdx.x >> 5) - Sh::kWarps;
-        if (role == 0) fetch_role<D>(sh, prm, bp, pv, &k_map, &v_map, &ks_map, &vs_map);
-        else if (role == 1) q_role<D>(sh, prm, bp, pv);
+        if (role == 3) q_role<D>(sh, prm, bp, pv);
+        else if (ring >= 0) fetch_role<D>(sh, ring, prm, bp, pv, &k_map, &v_map, &ks_map, &vs_map);
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWarps == 12 ? 152 : 224));
@@ -542,6 +583,11 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const Params& prm, const BlockP
 // rows x heads of a kv head: two M tiles of 16 at most
 bool block_register_supported(const confu_dims& d) { return (d.T + d.C) * (d.Hq / d.Hkv) <= 32; }
 
+// Whether the CTAs of a share are one per kv head: the rows of a slot's heads are neighbours in memory, and read at the same time they come from
+// DRAM as whole lines (the same loads without arithmetic: 4.8 TB/s head after head, 5.4 side by side).  Not where the heads would leave
+// more than a twentieth of the SMs without a share.
+bool block_by_heads(const confu_dims& d, int sm_count) { return d.Hkv > 1 && sm_count / d.Hkv * d.Hkv * 20 >= sm_count * 19; }
+
 cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache, const void* v_cache,
                                    int64_t n_slots, const SlotMap& map, const int32_t* prefix_len, const void* k_soft, const void* v_soft,
                                    const void* plan, void* partials, void* out, float* lse, int32_t* status, cudaStream_t st)
@@ -557,12 +603,12 @@ cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const vo
     prm.map = map;
     prm.prefix_len = prefix_len;
     prm.plan = plan;
-    prm.prefetch = 0;
+    prm.prefetch = plan != ctx->workspace;           // (where a call's own plan lies)
     prm.partials = (float*)partials;
     prm.out = (__nv_bfloat16*)out;
     prm.lse = lse;
     prm.status = status;
-    set_rows(prm, d, kPlanCta);
+    set_rows(prm, d, block_by_heads(d, ctx->sm_count) ? kPlanHeads : kPlanCta);
     prm.c = (d.sm_scale != 0.f ? d.sm_scale : 1.f / sqrtf((float)d.D)) * 1.4426950408889634f;
     prm.wait_ns = ctx->wait_ns;
     prm.k_scale = prm.v_scale = nullptr;

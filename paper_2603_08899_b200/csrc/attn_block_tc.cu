@@ -567,6 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
     const PlanView pv = plan_view(const_cast<void*>(prm.plan), prm.d.B, prm.d.Hkv);
+    if (prm.prefetch && threadIdx.x == 15 * 32) prefetch_lane<D, D>(prm, pv, &q_map, &k_map);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // 512 threads x 128 registers = 256 x 176 + 128 x 104 + 128 x 56
@@ -578,6 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         convert_role<D>(sh, prm);
     } else {
+        __syncwarp();                                // (warp 15, of which a lane has fetched ahead)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 12) {
             if (prm.n_mt > 1) mma_role<D, true>(sh, prm, pv, tmem);
@@ -639,7 +641,7 @@ cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const
     prm.map = map;
     prm.prefix_len = prefix_len;
     prm.plan = plan;
-    prm.prefetch = 0;
+    prm.prefetch = plan != ctx->workspace;           // (where a call's own plan lies)
     prm.partials = (float*)partials;
     prm.out = (__nv_bfloat16*)out;
     prm.lse = lse;

@@ -21,6 +21,7 @@ struct Params {
     int kind;            // PlanKind of the launch's work units: a plan for another kind is refused
     int n_mt;            // M tiles in use (2 unless one holds all rows)
     int n_rg;            // groups of query rows; a pair = (sequence, kv head, row group)
+    int side;            // CTAs that walk a share side by side: one per row group, or per kv head (kPlanHeads)
     int G;               // query heads per kv head
     int rpt;             // query rows per M tile (128 / G)
     int tpg;             // M tiles per row group
@@ -60,6 +61,7 @@ inline void set_rows(Params& p, const confu_dims& d, int kind)
     p.rpt = rows_per_tile(p.G);
     p.n_mt = d.T + d.C > p.rpt ? tpg : 1;
     p.n_rg = row_groups(d.T + d.C, p.G, tpg);
+    p.side = kind == kPlanHeads ? d.Hkv : p.n_rg;
 }
 
 // Enqueues the merge of the partial results that the attention launch with the same parameters

@@ -59,11 +59,11 @@ constexpr int kMergeThreads = 256, kMergeWarps = kMergeThreads / 32;
 
 struct Pair {
     int b, g, rg;
-    int c0, n;                 // first work unit and number of units that walked the pair (every n_rg-th from c0)
+    int c0, n;                 // first work unit and number of units that walked the pair (every `side`-th from c0)
 };
 __device__ __forceinline__ const float* part_of(const Params& prm, const Pair& u, int p)
 {
-    return prm.partials + (size_t)(2 * (u.c0 + p * prm.n_rg) + (p < u.n - 1 ? 1 : 0)) * (partial_slot_bytes() / sizeof(float));
+    return prm.partials + (size_t)(2 * (u.c0 + p * prm.side) + (p < u.n - 1 ? 1 : 0)) * (partial_slot_bytes() / sizeof(float));
 }
 // query row of row `lane_row` of M tile t (may be past the last)
 __device__ __forceinline__ int query_row(const Params& prm, const Pair& u, int t, int lane_row) { return prm.rpt * (prm.tpg * u.rg + t) + lane_row / prm.G; }
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(const Params pr
         if (prm.status && threadIdx.x == 0 && u.g == 0 && u.rg == 0 && blockIdx.y == 0 && blockIdx.z == 0) prm.status[u.b] = CONFU_ST_BAD_PLAN;
         return;
     }
-    u.c0 = parts.first() * prm.n_rg + u.rg;
+    u.c0 = parts.first() * prm.side + (prm.kind == kPlanHeads ? u.g : u.rg);
     u.n = parts.n();
     if (u.n == 1) return;                                   // one unit covered the pair and wrote the output itself
     const int rows = prm.rpt * prm.G;                       // of an M tile
@@ -202,7 +202,9 @@ cudaError_t launch_combine(const Params& prm, int units, cudaStream_t st)
     // 500..4000: 1 row 20.7 us, and 22.7 with the loads of rows that the warp does not have repeated instead of left out.
     const int n_pairs = prm.d.B * prm.d.Hkv * prm.n_rg, tiles = n_pairs * prm.n_mt;
     const int per_warp = tiles <= units ? 1 : tiles <= 2 * units ? 2 : 4;
-    const dim3 grid((unsigned)n_pairs, (unsigned)prm.n_mt, (unsigned)(128 / (kMergeWarps * per_warp)));
+    // (a step of few rows fills a part of its one M tile)
+    const int rows = (prm.d.T + prm.d.C < prm.rpt ? prm.d.T + prm.d.C : prm.rpt) * prm.G, per_block = kMergeWarps * per_warp;
+    const dim3 grid((unsigned)n_pairs, (unsigned)prm.n_mt, (unsigned)((rows + per_block - 1) / per_block));
     return prm.d.D == 64 ? launch_pdl(merge_kernel<64>, grid, dim3(kMergeThreads), st, prm, per_warp)
                          : launch_pdl(merge_kernel<kD>, grid, dim3(kMergeThreads), st, prm, per_warp);
 }

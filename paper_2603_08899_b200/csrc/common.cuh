@@ -31,8 +31,9 @@ __host__ __device__ inline int row_groups(int R, int G, int tiles_per_group)
 
 // The kinds of work units a plan can be for: CTAs that hold two M tiles (one row group = two tiles), CTA pairs (the same
 // rows, one tile per CTA), CTAs that hold one M tile (one row group = one tile), none (dims that only the CUDA-core kernel
-// takes: it reads the masks alone).
-enum PlanKind { kPlanCta = 0, kPlanPair = 1, kPlanNarrow = 2, kPlanMasks = 3 };
+// takes: it reads the masks alone), CTAs that hold the few rows of a kv head (one row group), a CTA of every share for each head: those read
+// neighbouring heads' rows of the same slots at the same time, whole lines of DRAM between them.
+enum PlanKind { kPlanCta = 0, kPlanPair = 1, kPlanNarrow = 2, kPlanMasks = 3, kPlanHeads = 4 };
 __host__ __device__ inline int tiles_per_group(int kind) { return kind == kPlanNarrow ? 1 : 2; }
 
 // ---------------------------------------------------------------------------

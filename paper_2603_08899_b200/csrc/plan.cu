@@ -63,6 +63,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
     static_assert(sizeof(s_mask) >= kPlanCached * sizeof(short2), "s_cut");
     PlanView pv = plan_view(plan_raw, B, d.Hkv);
     const bool cached = B <= kPlanCached;
+    // kv heads whose stretches follow one another on the line; by heads (kPlanHeads) there is one stretch per sequence and a CTA of each share per head
+    const int Hkv = kind == kPlanHeads ? 1 : d.Hkv;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
     if (kind == kPlanMasks) return;
     // ---- shares of their own, or the cost line: one stretch per (sequence, kv head); its groups of query rows are walked
     // side by side ----
-    const int n_rg = row_groups(R, d.Hq / d.Hkv, tiles_per_group(kind));
+    const int n_rg = kind == kPlanHeads ? d.Hkv : row_groups(R, d.Hq / d.Hkv, tiles_per_group(kind));
     if (warp == 0) {
         // The work is cut into `lanes` shares; CTA lane * n_rg + rg walks the lane's share for row group rg,
         // so the CTAs of a lane read the same K/V tiles at about the same time (the second read hits L2).
@@ -148,8 +150,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
             tiles = __reduce_add_sync(0xffffffffu, tiles);
             line = __reduce_add_sync(0xffffffffu, line);
             // (32 bits hold these sums, and the products with the heads but for absurd numbers of them)
-            if (!__any_sync(0xffffffffu, huge) && tiles && (uint64_t)line * d.Hkv < (1u << 30)) {
-                const uint32_t L = (uint32_t)lanes, H = (uint32_t)d.Hkv;
+            if (!__any_sync(0xffffffffu, huge) && tiles && (uint64_t)line * Hkv < (1u << 30)) {
+                const uint32_t L = (uint32_t)lanes, H = (uint32_t)Hkv;
                 int lo = (int)((tiles * H + L - 1) / L) + kRunOverheadTiles;         // no share is shorter than the mean
                 const int longest = (int)((line * H + L - 1) / L) + kRunOverheadTiles;
 // The shortest that fits.  Larger batches seldom have one, so the longest is tried first there: a search that goes all the way
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
                     }
                     uint32_t n = 0;
 #pragma unroll 1
-                    for (int b = lane; b < B; b += 32) n += (uint32_t)shares_of(s_tiles[b], at, d.Hkv).total;
+                    for (int b = lane; b < B; b += 32) n += (uint32_t)shares_of(s_tiles[b], at, Hkv).total;
                     if ((int)__reduce_add_sync(0xffffffffu, n) <= lanes) hi = at;
                     else lo = at + 1;
                 }
@@ -174,9 +176,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
         for (int b0 = 0; b0 < B; b0 += 32) {
             const int b = b0 + lane;
             const int tiles = b < B ? (cached ? s_tiles[b] : pv.tiles[b]) : 0;
-            int64_t mine = tiles > 0 ? (int64_t)(tiles + kPairOverheadTiles) * d.Hkv : 0;
+            int64_t mine = tiles > 0 ? (int64_t)(tiles + kPairOverheadTiles) * Hkv : 0;
             if (own) {
-                const Shares sh = shares_of(tiles, own, d.Hkv);
+                const Shares sh = shares_of(tiles, own, Hkv);
                 mine = sh.total;
                 if (b < B) s_cut[b] = make_short2((short)sh.pieces, (short)sh.whole);
             }
@@ -227,15 +229,15 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
     }
     if (s_own) {
         for (int u = tid; u < B * d.Hkv; u += (int)blockDim.x) {
-            const int b = u / d.Hkv, h = u % d.Hkv, pieces = s_cut[b].x, whole = s_cut[b].y;
+            const int b = u / d.Hkv, h = kind == kPlanHeads ? 0 : u % d.Hkv, pieces = s_cut[b].x, whole = s_cut[b].y;
             pv.parts[u] = Parts::make(pieces ? (int)s_base[b] + (whole > 1 ? h / whole : h * pieces) : 0, pieces, kind);
         }
         int n_runs = 0, begin = 0;
         if (c < n_ctas) {
             const int nt = s_tiles[seq0], local = c / n_rg - (int)s_base[seq0], pieces = s_cut[seq0].x, whole = s_cut[seq0].y;
             const int head = pieces > 1 ? local / pieces : local, p = local - head * pieces, head0 = head * whole;
-            n_runs = min(whole, d.Hkv - head0);
-            begin = (seq0 * d.Hkv + head0) * n_rg + c % n_rg * n_runs;       // (a share's runs have its stretches' places)
+            n_runs = min(whole, Hkv - head0);
+            begin = (seq0 * Hkv + head0) * n_rg + c % n_rg * n_runs;       // (a share's runs have its stretches' places)
             SegDesc s;
             s.b = seq0;
             s.t0 = pieces > 1 ? p * nt / pieces : 0;             // (256 pieces of 2^20 tiles at most)
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(confu_dims d, int un
         const int b = u / d.Hkv, nt = cached ? s_tiles[b] : pv.tiles[b];
         Parts parts = Parts::make(0, 0, kind);
         if (nt > 0) {
-            const int64_t F = base_of(b) + (int64_t)(u % d.Hkv) * (nt + kPairOverheadTiles) + kPairOverheadTiles;
+            const int64_t F = base_of(b) + (int64_t)(kind == kPlanHeads ? 0 : u % d.Hkv) * (nt + kPairOverheadTiles) + kPairOverheadTiles;
             const int lo = (int)(((F + 1) * n_lanes - 1) / N), hi = (int)(((F + nt) * n_lanes - 1) / N);
             parts = Parts::make(lo, hi - lo + 1, kind);
         }
