@@ -68,6 +68,7 @@ bool pair_attention_supported(const confu_dims& d);
 bool fp8_attention_supported(const confu_dims& d);
 bool block_register_supported(const confu_dims& d);
 bool block_by_heads(const confu_dims& d, int sm_count);
+bool block_one_tile(const confu_dims& d, int sm_count);
 cudaError_t launch_attention_fp8(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache,
                                  const void* v_cache, int64_t n_slots, const SlotMap& map,
                                  const int32_t* prefix_len, const void* k_soft, const void* v_soft, const void* plan,
@@ -148,7 +149,10 @@ int resolve_attention_path(const confu_ctx* ctx, const confu_dims& d)
 // row group: there have to be that many.  A path that the caller has chosen is taken as it is named.
 int plan_kind(const confu_ctx* ctx, const confu_dims& d, int path)
 {
-    if (d.kv_dtype == CONFU_FP8_BLOCK) return path == CONFU_ATTENTION_GENERIC && block_by_heads(d, ctx->sm_count) ? kPlanHeads : kPlanCta;
+    if (d.kv_dtype == CONFU_FP8_BLOCK) {
+        if (path == CONFU_ATTENTION_GENERIC) return block_by_heads(d, ctx->sm_count) ? kPlanHeads : kPlanCta;
+        return block_one_tile(d, ctx->sm_count) ? kPlanNarrow : kPlanCta;
+    }
     if (path == CONFU_ATTENTION_TENSOR_PAIR) return kPlanPair;
     if (path == CONFU_ATTENTION_GENERIC && !tc_attention_supported(d) && !pair_attention_supported(d)) return kPlanMasks;
     const int n_tiles = row_groups(d.T + d.C, d.Hq / d.Hkv, 1);

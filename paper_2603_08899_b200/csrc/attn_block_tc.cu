@@ -24,7 +24,7 @@ bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t h
 
 namespace blktc {
 
-// warps 0-3: softmax of M tile 0, 4-7: of M tile 1, 8-11: codes to f16, 12: MMA, 13: where the tiles are, 14: Q
+// warps 0-3: softmax of M tile 0, 4-7: of M tile 1 (with one M tile: of half 0 and half 1 of its keys), 8-11: codes to f16, 12: MMA, 13: where the tiles are, 14: Q
 constexpr int kThreads = 512;
 template <int D> constexpr int kTile = kTileKeys * D * 2;             // a 128-key tile as f16
 template <int D> constexpr int kStages = D == 128 ? 2 : 4;            // stage g = [V of the CTA's g-1st key tile | K of its g-th]
@@ -37,6 +37,7 @@ constexpr int kAhead = 8;                           // tiles that are known ahea
 constexpr int kScaleRing = 8;
 // f16 x f16 -> fp32 (formats 0), M = 128: N = 64 keys, B K-major; N = D, B MN-major
 constexpr uint32_t kIdescS = (1u << 4) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t kIdescS128 = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 template <int D> constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24);
 
 struct BlockParams {
@@ -67,6 +68,8 @@ struct SharedStorage {
     uint64_t scales_full[kScaleRing];
     uint64_t s_full[2][2], p_full[2][2], o_done[2];      // [M tile][half of the key tile]
     uint64_t pv0_done[2];                 // P V of half 0 of a run's last tile has completed
+    // one M tile: scores of a tile, per S buffer; weights, per S buffer and half; the run's accumulators have been read; the halves' statistics are there
+    uint64_t s_one[2], p_one[2][2], o_read, met;
     uint32_t tmem_base;
     int abort;
 };
@@ -102,7 +105,7 @@ __device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockP
         return true;
     };
     TileDesc d;
-    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s)) {
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s)) {
         const int32_t* table = prm.map.block_table + (size_t)s.b * prm.map.max_pages;
         for (int t0 = s.t0; t0 < s.t1; t0 += 8) {
             const int t = t0 + (lane >> 2);
@@ -140,12 +143,12 @@ __device__ void q_role(SharedStorage<D>& sh, const Params& prm, const PlanView& 
     Segment s;
     uint32_t seg = 0;
     const int R = prm.d.T + prm.d.C;
-    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s), ++seg) {
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s), ++seg) {
         if (!mbar_wait(&sh.q_empty, (seg & 1) ^ 1, &sh.abort, prm.wait_ns)) return;
         mbar_arrive_expect_tx(&sh.q_landed, (D / 64) * prm.n_mt * (uint32_t)(prm.rpt * prm.G) * 128u);
         for (int mt = 0; mt < prm.n_mt; ++mt)
             for (int kb = 0; kb < D / 64; ++kb)
-                tma_load_3d(sh.q + mt * kTile<D> + kb * kHalfTile, q_map, &sh.q_landed, kb * 64, s.g * prm.G, s.b * R + prm.rpt * (2 * s.rg + mt));
+                tma_load_3d(sh.q + mt * kTile<D> + kb * kHalfTile, q_map, &sh.q_landed, kb * 64, s.g * prm.G, s.b * R + prm.rpt * (prm.tpg * s.rg + mt));
     }
 }
 
@@ -229,10 +232,10 @@ __device__ void convert_role(SharedStorage<D>& sh, const Params& prm)
 }
 
 // One warp drives the tensor pipe, one lane of it issues: as in attn_tc.cu, without the wait for repaired rows.
-template <int D, bool kTwo>
+template <int D>
 __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem)
 {
-    constexpr int kMt = kTwo ? 2 : 1;
+    constexpr int kMt = 2;
     Walker w;
     Segment s;
     uint32_t stage = 0, seg = 0;
@@ -301,13 +304,82 @@ __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView
         prev_last = cur_last;
         return true;
     };
-    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s)) {
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s)) {
         const int n_tiles = s.t1 - s.t0;
         for (int j = 0; j < n_tiles; ++j)
             if (!run_stage(true, j == 0, j + 1 == n_tiles)) return;
         ++seg;
     }
     if (have_prev) run_stage(false, false, false);
+}
+
+// The same with one M tile: S of a tile in one of two buffers, each half of a tile's keys with an accumulator of its own.  Q K^T of tile g goes before
+// P V of tile g - 1, whose weights are being worked on meanwhile; where tile g starts a run, after it: the new Q is laid out by threads that
+// finish the old run first.
+template <int D>
+__device__ void mma_one_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem)
+{
+    Walker w;
+    Segment s;
+    uint32_t g = 0, seg = 0;                         // stages, runs
+    const bool issuer = elect_lane();
+    const uint32_t q_lo = desc_lo(smem_u32(sh.q), 16);
+    const uint32_t v_lo0 = desc_lo(smem_u32(sh.kv[0][0]), kHalfTile), k_lo0 = desc_lo(smem_u32(sh.kv[0][1]), 16);
+    constexpr uint32_t kStageStep = 2 * (kTile<D> >> 4);
+    auto issue_qk = [&](uint32_t kl) {
+        if (!issuer) return;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const uint32_t off = ((uint32_t)(i >> 2) * kHalfTile + (uint32_t)(i & 3) * 32u) >> 4;
+            mma_ss(tmem + (g & 1) * 128, q_lo + off, kl + off, kIdescS128, i > 0 ? 1u : 0u);
+        }
+        tc_commit(&sh.s_one[g & 1]);
+    };
+    auto issue_pv = [&](uint32_t vl, bool first, bool last, uint32_t run) -> bool {      // of tile g - 1, in run number `run`
+        // (the accumulators of the run before have been read by everybody)
+        if (first && run > 0 && !mbar_wait(&sh.o_read, (run - 1) & 1, &sh.abort, prm.wait_ns)) return false;
+        const uint32_t buf = (g - 1) & 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (!mbar_wait(&sh.p_one[buf][h], ((g - 1) >> 1) & 1, &sh.abort, prm.wait_ns)) return false;
+            tc_fence_after();
+            if (!issuer) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                mma_ts(tmem + 256 + h * 128, tmem + buf * 128 + h * 64 + i * 8, vl + (4 * h + i) * (2048u >> 4), kIdescO<D>, first && i == 0 ? 0u : 1u);
+        }
+        if (last && issuer) tc_commit(&sh.o_done[0]);
+        return true;
+    };
+    bool have_prev = false, prev_first = false;
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s), ++seg)
+        for (int t = s.t0; t < s.t1; ++t, ++g) {
+            const uint32_t st = g % kStages<D>;
+            if (!mbar_wait(&sh.kv_full[st], (g / kStages<D>) & 1, &sh.abort, prm.wait_ns)) return;
+            tc_fence_after();
+            const uint32_t vl = v_lo0 + st * kStageStep, kl = k_lo0 + st * kStageStep;
+            if (t == s.t0) {
+                if (have_prev && !issue_pv(vl, prev_first, true, seg - 1)) return;
+                if (!mbar_wait(&sh.q_full[0], seg & 1, &sh.abort, prm.wait_ns)) return;
+                tc_fence_after();
+                issue_qk(kl);
+            } else {
+                issue_qk(kl);
+                if (!issue_pv(vl, prev_first, false, seg)) return;
+            }
+            if (issuer) {
+                tc_commit(&sh.kv_empty[st]);
+                if (t + 1 == s.t1) tc_commit(&sh.q_empty);
+            }
+            have_prev = true;
+            prev_first = t == s.t0;
+        }
+    if (have_prev) {
+        const uint32_t st = g % kStages<D>;
+        if (!mbar_wait(&sh.kv_full[st], (g / kStages<D>) & 1, &sh.abort, prm.wait_ns)) return;
+        tc_fence_after();
+        issue_pv(v_lo0 + st * kStageStep, prev_first, true, seg - 1);
+    }
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
@@ -394,7 +466,7 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Plan
     Walker w;
     Segment s;
     uint32_t seg = 0, g = 0;                                // runs, tiles: s_full[t][half] completes once a tile
-    for (bool run = w.begin(pv, prm, blockIdx.x, kPlanCta, s); run; run = w.next(s)) {
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s)) {
         const int r = prm.rpt * (2 * s.rg + t) + lane_row / G;            // query row of this thread in this pair
         const bool row_valid = lane_row < prm.rpt * G && r < R;
         const uint64_t mask = row_valid ? pv.mask[(size_t)s.b * kMaxRows + r] : 0ull;
@@ -528,7 +600,156 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Plan
     }
 }
 
+// The softmax threads with one M tile: two warpgroups have the same rows and half of every tile's keys each, with a reference maximum, a sum and an
+// accumulator of its own; they meet once, at the end of a run.
 template <int D>
+__device__ void softmax_one_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem, int half)
+{
+    const int lane_row = threadIdx.x & 127, wq = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
+    const uint32_t s_addr = tmem + lane_base + 64 * half, o_addr = tmem + lane_base + 256 + 128 * half;
+    const int G = prm.G, T = prm.d.T, R = prm.d.T + prm.d.C, S = prm.d.S, Hq = prm.d.Hq;
+    const int hl = lane_row % G;
+    // (in the place of the second M tile)
+    float* q_scale = reinterpret_cast<float*>(sh.q + kTile<D>);                     // [row]
+    float2* stat = reinterpret_cast<float2*>(sh.q + kTile<D> + 512);                // [half][row]: reference maximum, sum of weights
+
+    Walker w;
+    Segment s;
+    uint32_t seg = 0, g = 0;                                // runs, tiles
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s)) {
+        const int r = prm.rpt * s.rg + lane_row / G;                      // query row of this thread in this run
+        const bool row_valid = lane_row < prm.rpt * G && r < R;
+        const uint64_t mask = row_valid ? pv.mask[(size_t)s.b * kMaxRows + r] : 0ull;
+        if (half == 0) {                                    // (every Q K^T of the run before has completed: its last scores have been seen)
+            if (!mbar_wait(&sh.q_landed, seg & 1, &sh.abort, prm.wait_ns)) return;
+            q_scale[lane_row] = prm.c * convert_q_row<D>(sh.q, row_valid, lane_row);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.q_full[0]);
+        } else if (!mbar_wait(&sh.q_full[0], seg & 1, &sh.abort, prm.wait_ns))
+            return;
+        const float c = q_scale[lane_row];
+        float m_ref = -INFINITY, l = 0.f;                   // of this half's keys
+        for (int tile = s.t0; tile < s.t1; ++tile, ++g) {
+            const uint32_t buf = g & 1;
+            if (!mbar_wait(&sh.scales_full[g % kScaleRing], (g / kScaleRing) & 1, &sh.abort, prm.wait_ns)) return;
+            const float4 sc0 = sh.scales[g % kScaleRing][2 * half], sc1 = sh.scales[g % kScaleRing][2 * half + 1];
+            if (!mbar_wait(&sh.s_one[buf], (g >> 1) & 1, &sh.abort, prm.wait_ns)) return;
+            tc_fence_after();
+            uint32_t sv[64];
+            tmem_ld32(s_addr + buf * 128, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+            tmem_ld32(s_addr + buf * 128 + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+            tc_wait_ld();
+            if (tile >= s.masked) {
+                uint64_t lo, hi;
+                visible_bits(s, tile, R, T, S, r, row_valid, mask, lo, hi);
+                const uint64_t vis = half ? hi : lo;
+#pragma unroll
+                for (int j = 0; j < 64; ++j)
+                    if (!((vis >> j) & 1ull)) sv[j] = 0xff800000u;               // -inf
+            }
+            const float a0 = fmaxf(c * sc0.x, 1.1754944e-38f), a1 = fmaxf(c * sc1.x, 1.1754944e-38f);
+            const float m_new = fmaxf(m_ref, fmaxf(fmaf(max32(sv), a0, sc0.y), fmaf(max32(sv + 32), a1, sc1.y)));
+            if (tile == s.t0)
+                m_ref = m_new;
+            else {
+                const bool move = m_new - m_ref > kRescaleThreshold;             // false when both are -inf (NaN)
+                if (__any_sync(0xffffffffu, move)) {
+                    // P V of the tile before has completed when stage g of the ring is free again.  (That cannot happen twice before this thread
+                    // has handed this tile's weights over: the parity is enough, though not every phase is waited for here.)
+                    if (!mbar_wait(&sh.kv_empty[g % kStages<D>], (g / kStages<D>) & 1, &sh.abort, prm.wait_ns)) return;
+                    tc_fence_after();
+                    const float alpha = move ? ex2(m_ref - m_new) : 1.f;
+                    if (move) { m_ref = m_new; l *= alpha; }
+#pragma unroll 1
+                    for (int q4 = 0; q4 < D / 16; ++q4) {
+                        uint32_t ov[16];
+                        tmem_ld16(o_addr + q4 * 16, ov);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) ov[j] = __float_as_uint(__uint_as_float(ov[j]) * alpha);
+                        tmem_st16(o_addr + q4 * 16, ov);
+                    }
+                }
+            }
+            const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
+            uint32_t pk[16];
+            l = fmaf(weights32(sv, a0, sc0.y + neg_m, pk), sc0.z, l);
+            tmem_st16(s_addr + buf * 128, pk);
+            l = fmaf(weights32(sv + 32, a1, sc1.y + neg_m, pk), sc1.z, l);
+            tmem_st16(s_addr + buf * 128 + 16, pk);
+            tc_wait_st();
+            tc_fence_before();
+            mbar_arrive(&sh.p_one[buf][half]);
+        }
+        // ---- end of the run, while the last P V goes on: the halves' sums, at the larger (= the row's) reference maximum ----
+        stat[half * 128 + lane_row] = make_float2(m_ref, l);
+        mbar_arrive(&sh.met);
+        if (!mbar_wait(&sh.met, seg & 1, &sh.abort, prm.wait_ns)) return;
+        const float2 other = stat[(half ^ 1) * 128 + lane_row];
+        const float m_row = fmaxf(m_ref, other.x);
+        const float a_me = m_ref == -INFINITY ? 0.f : ex2(m_ref - m_row), a_ot = other.x == -INFINITY ? 0.f : ex2(other.x - m_row);
+        const float l_row = half ? other.y * a_ot + l * a_me : l * a_me + other.y * a_ot;       // (the same number in both)
+        const bool whole = s.part_slot < 0;
+        const float inv_l = whole ? 1.f / l_row : 1.f;
+        const float f0 = (half ? a_ot : a_me) * inv_l, f1 = (half ? a_me : a_ot) * inv_l;
+        float4* xp = sh.xpose[threadIdx.x >> 5];
+        __nv_bfloat16* o_ptr[4];
+        float* p_ptr = nullptr;
+        if (whole) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                const int lr = wq * 32 + 8 * kk + (lane >> 2);
+                const int rk = prm.rpt * s.rg + lr / G;
+                o_ptr[kk] = (lr < prm.rpt * G && rk < R) ? prm.out + (((size_t)s.b * R + rk) * Hq + s.g * G + lr % G) * D + 8 * (lane & 3) : nullptr;
+            }
+            if (half == 0 && row_valid && prm.lse) prm.lse[((size_t)s.b * R + r) * Hq + s.g * G + hl] = natural_lse(m_row, l_row);
+        } else {
+            float* part = prm.partials + (size_t)s.part_slot * (partial_slot_bytes() / sizeof(float));
+            p_ptr = part + (size_t)(wq * 32 + (lane >> 3)) * kPartD + 4 * (lane & 7);
+            if (half == 0) {
+                part[(size_t)kPartRows * kPartD + lane_row] = m_row;
+                part[(size_t)kPartRows * kPartD + kPartRows + lane_row] = l_row;
+            }
+        }
+        if (!mbar_wait(&sh.o_done[0], seg & 1, &sh.abort, prm.wait_ns)) return;
+        tc_fence_after();
+        constexpr int kChunks = D / 64;                      // of 32 columns; this half's warps write D / 2 columns
+#pragma unroll 1
+        for (int q4 = kChunks * half; q4 < kChunks * half + kChunks; ++q4) {
+            uint32_t u0[32], u1[32];
+            tmem_ld32(tmem + lane_base + 256 + q4 * 32, u0);
+            tmem_ld32(tmem + lane_base + 384 + q4 * 32, u1);
+            tc_wait_ld();
+            auto sum = [&](int i) { return fmaf(__uint_as_float(u0[i]), f0, __uint_as_float(u1[i]) * f1); };
+#pragma unroll
+            for (int q = 0; q < 8; ++q) xp[lane * 8 + (q ^ (lane & 7))] = make_float4(sum(4 * q), sum(4 * q + 1), sum(4 * q + 2), sum(4 * q + 3));
+            __syncwarp();
+            if (whole) {
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) {
+                    const int k = 8 * kk + (lane >> 2), q = 2 * (lane & 3);
+                    const float4 a = xp[k * 8 + (q ^ (k & 7))], b2 = xp[k * 8 + ((q + 1) ^ (k & 7))];
+                    if (o_ptr[kk])
+                        *reinterpret_cast<uint4*>(o_ptr[kk] + q4 * 32) =
+                            make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b2.x, b2.y), pack_bf16(b2.z, b2.w));
+                }
+            } else {
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) {
+                    const int k = 4 * kk + (lane >> 3);
+                    *reinterpret_cast<float4*>(p_ptr + (size_t)(4 * kk) * kPartD + q4 * 32) = xp[k * 8 + ((lane & 7) ^ (k & 7))];
+                }
+            }
+            __syncwarp();
+        }
+        tc_fence_before();
+        mbar_arrive(&sh.o_read);
+        ++seg;
+    }
+}
+
+template <int D, bool kOne>
 __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const Params prm, const BlockParams bp)
 {
@@ -551,7 +772,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
             }
             mbar_init(&sh.o_done[t], 1);
             mbar_init(&sh.pv0_done[t], 1);
+            mbar_init(&sh.s_one[t], 1);
+            for (int h = 0; h < 2; ++h) mbar_init(&sh.p_one[t][h], 128);
         }
+        mbar_init(&sh.o_read, 256);
+        mbar_init(&sh.met, 256);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -574,7 +799,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int t = warp >> 2;
-        if (t < prm.n_mt) softmax_role<D>(sh, prm, pv, tmem, t);
+        if constexpr (kOne) softmax_one_role<D>(sh, prm, pv, tmem, t);
+        else if (t < prm.n_mt) softmax_role<D>(sh, prm, pv, tmem, t);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         convert_role<D>(sh, prm);
@@ -582,8 +808,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
         __syncwarp();                                // (warp 15, of which a lane has fetched ahead)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 12) {
-            if (prm.n_mt > 1) mma_role<D, true>(sh, prm, pv, tmem);
-            else mma_role<D, false>(sh, prm, pv, tmem);
+            if constexpr (kOne) mma_one_role<D>(sh, prm, pv, tmem);
+            else mma_role<D>(sh, prm, pv, tmem);
         } else if (warp == 13)
             tiles_role<D>(sh, prm, bp, pv, &k_map, &v_map);
         else if (warp == 14) {
@@ -608,12 +834,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
     }
 }
 
-template <int D>
+template <int D, bool kOne>
 cudaError_t launch(const CUtensorMap (&maps)[3], const Params& prm, const BlockParams& bp, int units, cudaStream_t st)
 {
-    const size_t smem = sizeof(SharedStorage<D>) + 1024;
+    constexpr size_t smem = sizeof(SharedStorage<D>) + 1024;
+    static_assert(smem <= 227 * 1024, "shared memory of a CTA");
     static OncePerDevice attr_done;
-    cudaError_t e = attr_done.run([&] { return cudaFuncSetAttribute(attention_block_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+    cudaError_t e = attr_done.run([&] { return cudaFuncSetAttribute(attention_block_tc_kernel<D, kOne>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute pdl[1];
     pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -625,11 +852,19 @@ cudaError_t launch(const CUtensorMap (&maps)[3], const Params& prm, const BlockP
     cfg.stream = st;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_block_tc_kernel<D>, maps[0], maps[1], maps[2], prm, bp);
+    return cudaLaunchKernelEx(&cfg, attention_block_tc_kernel<D, kOne>, maps[0], maps[1], maps[2], prm, bp);
 }
 
 }  // namespace blktc
 }  // namespace tc
+
+// Whether a CTA works on one M tile, its two warpgroups on half of the keys of every tile each: where one holds the rows, and where (sequence, kv
+// head, M tile) triples are few for the SMs, as for a bf16 cache.
+bool block_one_tile(const confu_dims& d, int sm_count)
+{
+    const int n_tiles = row_groups(d.T + d.C, d.Hq / d.Hkv, 1);
+    return sm_count >= n_tiles && (n_tiles == 1 || 2 * (int64_t)d.B * d.Hkv * n_tiles <= 3 * (int64_t)sm_count);
+}
 
 cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const void* q, const void* k_cache, const void* v_cache,
                                       int64_t n_slots, const SlotMap& map, const int32_t* prefix_len, const void* k_soft, const void* v_soft,
@@ -646,7 +881,7 @@ cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const
     prm.out = (__nv_bfloat16*)out;
     prm.lse = lse;
     prm.status = status;
-    set_rows(prm, d, kPlanCta);
+    set_rows(prm, d, block_one_tile(d, ctx->sm_count) ? kPlanNarrow : kPlanCta);
     prm.c = (d.sm_scale != 0.f ? d.sm_scale : 1.f / sqrtf((float)d.D)) * 1.4426950408889634f;
     prm.wait_ns = ctx->wait_ns;
     prm.k_scale = prm.v_scale = nullptr;
@@ -665,9 +900,11 @@ cudaError_t launch_attention_block_tc(const Ctx* ctx, const confu_dims& d, const
     if (!make_tile_map(&maps[0], q, (uint64_t)d.B * (d.T + d.C), d.Hq, prm.rpt, prm.G, d.D) || !make_code_map(&maps[1], k_cache, n_slots, d.Hkv, kTileKeys, d.D) ||
         !make_code_map(&maps[2], v_cache, n_slots, d.Hkv, kTileKeys, d.D))
         return cudaErrorInvalidValue;
-    const cudaError_t e = d.D == 64 ? blktc::launch<64>(maps, prm, bp, ctx->sm_count, st) : blktc::launch<128>(maps, prm, bp, ctx->sm_count, st);
+    const bool one = prm.kind == kPlanNarrow;
+    auto launch = d.D == 64 ? (one ? blktc::launch<64, true> : blktc::launch<64, false>) : (one ? blktc::launch<128, true> : blktc::launch<128, false>);
+    const cudaError_t e = launch(maps, prm, bp, ctx->sm_count, st);
     if (e != cudaSuccess) return e;
-    return launch_combine(prm, ctx->sm_count, st);
+    return launch_combine(prm, one ? ctx->sm_count / 2 : ctx->sm_count, st);
 }
 
 }  // namespace confu
