@@ -63,7 +63,7 @@ struct SharedStorage {
     TileDesc tiles[kAhead];
     float4 scales[kScaleRing][4];
     alignas(8) uint64_t q_landed, q_empty, q_full[2];
-    uint64_t tile_full[kAhead], tile_empty[kAhead];
+    uint64_t tile_full[kAhead], tile_scaled[kAhead], tile_empty[kAhead];
     uint64_t kv_full[kStages<D>], kv_empty[kStages<D>];
     uint64_t scales_full[kScaleRing];
     uint64_t s_full[2][2], p_full[2][2], o_done[2];      // [M tile][half of the key tile]
@@ -84,23 +84,26 @@ __device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockP
     Walker w;
     Segment s;
     uint32_t g = 0;
-    auto put = [&](int j, const TileDesc& d, const float4& scale) -> bool {       // the lanes of tile j of eight
+    auto put = [&](int j, const TileDesc& d, const float2& scale) -> bool {       // the lanes of tile j of eight
         const uint32_t e = g % kAhead;
         if (!__all_sync(0xffffffffu, mbar_wait(&sh.tile_empty[e], ((g / kAhead) & 1) ^ 1, &sh.abort, prm.wait_ns))) return false;
         if ((lane >> 2) == j) {
-            sh.tiles[e].scales[sub] = scale;
             if (sub == 0) {
                 sh.tiles[e].k = d.k;
                 sh.tiles[e].v = d.v;
                 sh.tiles[e].valid = d.valid;
-                if (d.z >= 0) {
+                mbar_arrive(&sh.tile_full[e]);
+                if (g > 0 && d.z >= 0) {             // (the first is loaded at once)
                     tma_prefetch_3d(k_map, 0, d.g, d.z);
                     tma_prefetch_3d(v_map, 0, d.g, d.z);
                 }
             }
+            // (read after the pages; the converting warps have begun by the time that these are here)
+            const float vs = fmaxf(scale.y, kLeastScale);
+            sh.tiles[e].scales[sub] = make_float4(scale.x, log2f(vs), 1.f / vs, 0.f);
+            mbar_arrive(&sh.tile_scaled[e]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.tile_full[e]);
         ++g;
         return true;
     };
@@ -123,16 +126,16 @@ __device__ void tiles_role(SharedStorage<D>& sh, const Params& prm, const BlockP
             if (sub * 32 < d.valid) {
                 const size_t sc = ((size_t)(soft ? 0 : page) * Hkv + s.g) * nb + sub * 32 / bp.block;
                 ks = __ldg((soft ? bp.ks_soft : bp.ks) + sc);
-                vs = fmaxf(__ldg((soft ? bp.vs_soft : bp.vs) + sc), kLeastScale);
+                vs = __ldg((soft ? bp.vs_soft : bp.vs) + sc);
             }
-            const float4 scale = make_float4(ks, log2f(vs), 1.f / vs, 0.f);
+            const float2 scale = make_float2(ks, vs);
             for (int j = 0; j < 8 && t0 + j < s.t1; ++j)
                 if (!put(j, d, scale)) return;
         }
     }
     d.k = d.v = nullptr;
     d.valid = d.z = -1;
-    put(0, d, make_float4(1.f, 0.f, 1.f, 0.f));
+    put(0, d, make_float2(1.f, 1.f));
 }
 
 // Q of a run, bf16, as soon as the last product of the run before has read that one's.
@@ -209,22 +212,20 @@ __device__ void convert_role(SharedStorage<D>& sh, const Params& prm)
     for (uint32_t g = 0;; ++g) {
         const uint32_t st = g % kStages<D>, e = g % kAhead;
         if (!mbar_wait(&sh.kv_empty[st], ((g / kStages<D>) & 1) ^ 1, &sh.abort, prm.wait_ns)) return;
-        if (g > 0) {
-            v.store(sh.kv[st][0], tid);
-            if (valid >= 0) v.load(sh.tiles[e].v, valid, pitch, tid);
-        }
-        if (valid >= 0) {
-            k.store(sh.kv[st][1], tid);
-            if (tid < 4) {
-                sh.scales[g % kScaleRing][tid] = sh.tiles[e].scales[tid];
-                mbar_arrive(&sh.scales_full[g % kScaleRing]);
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.tile_empty[e]);
-        }
+        if (g > 0) v.store(sh.kv[st][0], tid);
+        if (valid >= 0) k.store(sh.kv[st][1], tid);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&sh.kv_full[st]);
         if (valid < 0) return;                       // the last stage: V of the last tile, no K
+        // (loads behind the fence: it would wait for them)
+        if (g > 0) v.load(sh.tiles[e].v, valid, pitch, tid);
+        if (tid < 4) {
+            if (!mbar_wait(&sh.tile_scaled[e], (g / kAhead) & 1, &sh.abort, prm.wait_ns)) return;
+            sh.scales[g % kScaleRing][tid] = sh.tiles[e].scales[tid];
+            mbar_arrive(&sh.scales_full[g % kScaleRing]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.tile_empty[e]);
         if (!mbar_wait(&sh.tile_full[(g + 1) % kAhead], ((g + 1) / kAhead) & 1, &sh.abort, prm.wait_ns)) return;
         valid = sh.tiles[(g + 1) % kAhead].valid;
         if (valid >= 0) k.load(sh.tiles[(g + 1) % kAhead].k, valid, pitch, tid);
@@ -762,7 +763,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
         mbar_init(&sh.q_empty, 1);
         // a stage is full when every converting thread has written its pieces, free again when its MMAs have completed
         for (int i = 0; i < kStages<D>; ++i) { mbar_init(&sh.kv_full[i], 128); mbar_init(&sh.kv_empty[i], 1); }
-        for (int i = 0; i < kAhead; ++i) { mbar_init(&sh.tile_full[i], 1); mbar_init(&sh.tile_empty[i], 4); }
+        for (int i = 0; i < kAhead; ++i) { mbar_init(&sh.tile_full[i], 1); mbar_init(&sh.tile_scaled[i], 4); mbar_init(&sh.tile_empty[i], 4); }
         for (int i = 0; i < kScaleRing; ++i) mbar_init(&sh.scales_full[i], 4);
         for (int t = 0; t < 2; ++t) {
             mbar_init(&sh.q_full[t], 128);
