@@ -38,6 +38,7 @@ constexpr float kRescaleThreshold = 8.f;             // the reference maximum fo
 constexpr float kLeastScale = 7.8886091e-31f;        // 2^-100: no block has less
 
 struct BlockParams {
+    const uint8_t *v, *v_soft;
     const float *ks, *vs, *ks_soft, *vs_soft;
     const __nv_bfloat16* q;
     int64_t n_pages;
@@ -61,6 +62,7 @@ struct SharedStorage {
     float q_scale[kMt * 16];
     uint64_t mask[kMt * 16];
     alignas(8) uint64_t full[kWarps][kSlots], empty[kWarps][kSlots], q_full, q_empty, met;
+    int nan_run[2];                                  // of run number n, at n % 2: n + 1 where values that are not numbers were taken out
     int abort;
 };
 
@@ -251,7 +253,7 @@ __device__ void q_role(Sh& sh, const Params& prm, const BlockParams& bp, const P
 }
 
 template <int D, typename Sh>
-__device__ void consumer_role(Sh& sh, const Params& prm, const PlanView& pv)
+__device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
 {
     constexpr int kMt = Sh::kMt;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -301,6 +303,27 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const PlanView& pv)
             if (ok) {
                 const uint8_t *k_tile = sh.kv[warp][at.slot][0], *v_tile = sh.kv[warp][at.slot][1];
                 const float4 scale = sh.scales[warp][at.slot];
+                // A value that is not a number must not reach the rows that do not see its key, and 0 times it would.  Where not every row sees every key
+                // such codes are taken out; whose NaN they are is found out at the end of the run.
+                if (t >= s.masked) {
+                    uint4* piece = reinterpret_cast<uint4*>(sh.kv[warp][at.slot][1]) + lane;
+                    uint32_t trace = 0u;
+#pragma unroll
+                    for (int k = 0; k < Sh::kCodes / 512; ++k) {
+                        const uint4 c = piece[32 * k];
+                        trace |= e4m3_nan_trace(c.x) | e4m3_nan_trace(c.y) | e4m3_nan_trace(c.z) | e4m3_nan_trace(c.w);
+                    }
+                    if (__any_sync(0xffffffffu, (trace & kNanTrace) != 0u)) {
+                        sh.nan_run[seg & 1] = (int)seg + 1;
+#pragma unroll 1
+                        for (int k = 0; k < Sh::kCodes / 512; ++k) {
+                            const uint4 c = piece[32 * k];
+                            piece[32 * k] = make_uint4(c.x & ~e4m3_nan4(c.x), c.y & ~e4m3_nan4(c.y), c.z & ~e4m3_nan4(c.z), c.w & ~e4m3_nan4(c.w));
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the slot is filled by copies again)
+                        __syncwarp();
+                    }
+                }
                 // ---- scores ----
                 float sc[kMt][4][4];
 #pragma unroll
@@ -486,6 +509,27 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const PlanView& pv)
                     acc.w = fmaf(f, y.w, acc.w);
                 }
                 const int r = r0 + m / G;
+                if (*reinterpret_cast<volatile int*>(&sh.nan_run[seg & 1]) == (int)seg + 1) {
+                    // codes that are not numbers were taken out of this run: the row's four columns of all keys that it sees, again
+                    uint32_t nm = 0u;
+#pragma unroll 1
+                    for (int t = max(s.t0, s.masked); t < s.t1; ++t) {
+                        const bool soft = t >= s.nkt;
+                        const int page = soft ? 0 : __ldg(prm.map.block_table + (size_t)s.b * prm.map.max_pages + t);
+                        if ((uint32_t)page >= (uint64_t)bp.n_pages) continue;
+                        uint64_t lo, hi;
+                        visible_bits(s, t, R, T, S, r, true, pv.mask[(size_t)s.b * kMaxRows + r], lo, hi);
+                        const uint8_t* from = (soft ? bp.v_soft : bp.v) + ((size_t)page * kTileKeys * prm.d.Hkv + s.g) * D + 4 * v;
+#pragma unroll 1
+                        for (int key = 0; key < kTileKeys; ++key)
+                            if (((key < 64 ? lo : hi) >> (key & 63)) & 1ull) nm |= e4m3_nan4(__ldg(reinterpret_cast<const uint32_t*>(from + (size_t)key * prm.d.Hkv * D)));
+                    }
+                    const float nan = __int_as_float(0x7fffffff);
+                    if (nm & 0xffu) acc.x = nan;
+                    if (nm & 0xff00u) acc.y = nan;
+                    if (nm & 0xff0000u) acc.z = nan;
+                    if (nm & 0xff000000u) acc.w = nan;
+                }
                 if (whole) {
                     const size_t row_out = ((size_t)s.b * R + r) * Hq + s.g * G + m % G;
                     const float inv = 1.f / L;
@@ -524,6 +568,7 @@ attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         mbar_init(&sh.q_full, 1);
         mbar_init(&sh.q_empty, Sh::kWarps);
         mbar_init(&sh.met, Sh::kWarps);
+        sh.nan_run[0] = sh.nan_run[1] = 0;
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -543,7 +588,7 @@ attention_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWarps == 12 ? 152 : 224));
-        consumer_role<D>(sh, prm, pv);
+        consumer_role<D>(sh, prm, bp, pv);
     }
     __syncthreads();
     if (sh.abort) {
@@ -613,6 +658,8 @@ cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const vo
     prm.wait_ns = ctx->wait_ns;
     prm.k_scale = prm.v_scale = nullptr;
     blk::BlockParams bp;
+    bp.v = (const uint8_t*)v_cache;
+    bp.v_soft = (const uint8_t*)v_soft;
     bp.ks = ctx->k_block_scale;
     bp.vs = ctx->v_block_scale;
     bp.ks_soft = ctx->k_soft_scale;

@@ -24,7 +24,7 @@ bool make_code_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t h
 
 namespace blktc {
 
-// warps 0-3: softmax of M tile 0, 4-7: of M tile 1 (with one M tile: of half 0 and half 1 of its keys), 8-11: codes to f16, 12: MMA, 13: where the tiles are, 14: Q
+// warps 0-3: softmax of M tile 0, 4-7: of M tile 1 (with one M tile: of half 0 and half 1 of its keys), 8-11: codes to f16, 12: MMA, 13: where the tiles are, 14: Q, 15: NaN
 constexpr int kThreads = 512;
 template <int D> constexpr int kTile = kTileKeys * D * 2;             // a 128-key tile as f16
 template <int D> constexpr int kStages = D == 128 ? 2 : 4;            // stage g = [V of the CTA's g-1st key tile | K of its g-th]
@@ -70,6 +70,9 @@ struct SharedStorage {
     uint64_t pv0_done[2];                 // P V of half 0 of a run's last tile has completed
     // one M tile: scores of a tile, per S buffer; weights, per S buffer and half; the run's accumulators have been read; the halves' statistics are there
     uint64_t s_one[2], p_one[2][2], o_read, met;
+    uint64_t scan_full[2], scan_empty[2];
+    int scan_nan[2];                      // V of the tile has codes that are not numbers
+    int nan_run[8];                       // of run number n, at n % 8: n + 1 where such values were taken out
     uint32_t tmem_base;
     int abort;
 };
@@ -232,6 +235,65 @@ __device__ void convert_role(SharedStorage<D>& sh, const Params& prm)
     }
 }
 
+// 0 times a value that is not a number would reach the rows that do not see its key.  One warp looks for such codes in V of the tiles of which not
+// every row sees every key, well ahead of their products; the issuing warp then takes them out before the product, and whose NaN they
+// are is found out at the end of the run.  (By the converting warps the look took registers that the loads in flight want: 7 % of a chain's time.)
+template <int D>
+__device__ void scan_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv)
+{
+    constexpr int kPieces = D / 16, kRows = 32 / kPieces;
+    const int lane = threadIdx.x & 31;
+    const size_t pitch = (size_t)prm.d.Hkv * D;
+    Walker w;
+    Segment s;
+    uint32_t i = 0;
+    for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s))
+        for (int t = max(s.t0, s.masked); t < s.t1; ++t, ++i) {
+            const bool soft = t >= s.nkt;
+            const int page = soft ? 0 : __ldg(prm.map.block_table + (size_t)s.b * prm.map.max_pages + t);
+            const int valid = soft ? prm.d.S : (uint32_t)page < (uint64_t)bp.n_pages ? s.P + prm.d.T + prm.d.C - t * kTileKeys : 0;
+            const uint8_t* v = (soft ? bp.v_soft : bp.v) + (size_t)(valid ? page : 0) * kTileKeys * pitch + s.g * D + (lane % kPieces) * 16 + (lane / kPieces) * pitch;
+            uint32_t trace = 0u;
+#pragma unroll 1
+            for (int r0 = lane / kPieces; r0 < valid && r0 < kTileKeys; r0 += 4 * kRows, v += 4 * kRows * pitch) {
+                uint4 c[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    c[k] = make_uint4(0u, 0u, 0u, 0u);
+                    if (r0 + k * kRows < valid)
+                        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c[k].x), "=r"(c[k].y), "=r"(c[k].z), "=r"(c[k].w) : "l"(v + k * kRows * pitch));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) trace |= e4m3_nan_trace(c[k].x) | e4m3_nan_trace(c[k].y) | e4m3_nan_trace(c[k].z) | e4m3_nan_trace(c[k].w);
+            }
+            const bool nan = __any_sync(0xffffffffu, (trace & kNanTrace) != 0u);
+            if (!__all_sync(0xffffffffu, mbar_wait(&sh.scan_empty[i & 1], ((i >> 1) & 1) ^ 1, &sh.abort, prm.wait_ns))) return;
+            if (lane == 0) {
+                sh.scan_nan[i & 1] = nan;
+                mbar_arrive(&sh.scan_full[i & 1]);
+            }
+        }
+}
+
+// The issuing warp's side, before P V of a tile of which not every row sees every key: f16 values that are not numbers as zeros.
+template <int D>
+__device__ bool clean_tile(SharedStorage<D>& sh, const Params& prm, uint8_t* tile, uint32_t i, uint32_t run)
+{
+    if (!__all_sync(0xffffffffu, mbar_wait(&sh.scan_full[i & 1], (i >> 1) & 1, &sh.abort, prm.wait_ns))) return false;
+    if (sh.scan_nan[i & 1]) {
+#pragma unroll 1
+        for (int at = threadIdx.x & 31; at < kTile<D> / 4; at += 32) {
+            uint32_t* x = reinterpret_cast<uint32_t*>(tile) + at;
+            *x &= ~__vcmpgtu2(*x & 0x7fff7fffu, 0x7c007c00u);
+        }
+        sh.nan_run[run % 8] = (int)run + 1;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.scan_empty[i & 1]);
+    return true;
+}
+
 // One warp drives the tensor pipe, one lane of it issues: as in attn_tc.cu, without the wait for repaired rows.
 template <int D>
 __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem)
@@ -239,7 +301,7 @@ __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView
     constexpr int kMt = 2;
     Walker w;
     Segment s;
-    uint32_t stage = 0, seg = 0;
+    uint32_t stage = 0, seg = 0, looked = 0;         // stages, runs, tiles that were looked through for NaN
     const bool issuer = elect_lane();
     const uint32_t q_lo = desc_lo(smem_u32(sh.q), 16);
     const uint32_t v_lo0 = desc_lo(smem_u32(sh.kv[0][0]), kHalfTile), k_lo0 = desc_lo(smem_u32(sh.kv[0][1]), 16);
@@ -263,12 +325,13 @@ __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView
             mma_ts(tmem + 256 + t * 128, tmem + t * 128 + h * 64 + i * 8, vl + (4 * h + i) * (2048u >> 4), kIdescO<D>,
                    (first_of_run && h == 0 && i == 0) ? 0u : 1u);
     };
-    bool have_prev = false, prev_first = false, prev_last = false;
-    auto run_stage = [&](bool have_cur, bool cur_first, bool cur_last) -> bool {
+    bool have_prev = false, prev_first = false, prev_last = false, prev_masked = false;
+    auto run_stage = [&](bool have_cur, bool cur_first, bool cur_last, bool cur_masked) -> bool {
         const uint32_t st = stage % kStages<D>;
         if (!mbar_wait(&sh.kv_full[st], (stage / kStages<D>) & 1, &sh.abort, prm.wait_ns)) return false;
         tc_fence_after();
         const uint32_t vl = v_lo0 + st * kStageStep, kl = k_lo0 + st * kStageStep;
+        if (prev_masked && !clean_tile(sh, prm, sh.kv[st][0], looked++, prev_last ? seg - 1 : seg)) return false;
         if (have_prev) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -303,15 +366,16 @@ __device__ void mma_role(SharedStorage<D>& sh, const Params& prm, const PlanView
         have_prev = have_cur;
         prev_first = cur_first;
         prev_last = cur_last;
+        prev_masked = cur_masked;
         return true;
     };
     for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s)) {
         const int n_tiles = s.t1 - s.t0;
         for (int j = 0; j < n_tiles; ++j)
-            if (!run_stage(true, j == 0, j + 1 == n_tiles)) return;
+            if (!run_stage(true, j == 0, j + 1 == n_tiles, s.t0 + j >= s.masked)) return;
         ++seg;
     }
-    if (have_prev) run_stage(false, false, false);
+    if (have_prev) run_stage(false, false, false, false);
 }
 
 // The same with one M tile: S of a tile in one of two buffers, each half of a tile's keys with an accumulator of its own.  Q K^T of tile g goes before
@@ -322,7 +386,7 @@ __device__ void mma_one_role(SharedStorage<D>& sh, const Params& prm, const Plan
 {
     Walker w;
     Segment s;
-    uint32_t g = 0, seg = 0;                         // stages, runs
+    uint32_t g = 0, seg = 0, looked = 0;             // stages, runs, tiles that were looked through for NaN
     const bool issuer = elect_lane();
     const uint32_t q_lo = desc_lo(smem_u32(sh.q), 16);
     const uint32_t v_lo0 = desc_lo(smem_u32(sh.kv[0][0]), kHalfTile), k_lo0 = desc_lo(smem_u32(sh.kv[0][1]), 16);
@@ -336,9 +400,10 @@ __device__ void mma_one_role(SharedStorage<D>& sh, const Params& prm, const Plan
         }
         tc_commit(&sh.s_one[g & 1]);
     };
-    auto issue_pv = [&](uint32_t vl, bool first, bool last, uint32_t run) -> bool {      // of tile g - 1, in run number `run`
+    auto issue_pv = [&](uint32_t vl, bool first, bool last, bool masked, uint32_t run) -> bool {      // of tile g - 1, in run number `run`
         // (the accumulators of the run before have been read by everybody)
         if (first && run > 0 && !mbar_wait(&sh.o_read, (run - 1) & 1, &sh.abort, prm.wait_ns)) return false;
+        if (masked && !clean_tile(sh, prm, sh.kv[g % kStages<D>][0], looked++, run)) return false;
         const uint32_t buf = (g - 1) & 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -352,7 +417,7 @@ __device__ void mma_one_role(SharedStorage<D>& sh, const Params& prm, const Plan
         if (last && issuer) tc_commit(&sh.o_done[0]);
         return true;
     };
-    bool have_prev = false, prev_first = false;
+    bool have_prev = false, prev_first = false, prev_masked = false;
     for (bool run = w.begin(pv, prm, blockIdx.x, prm.kind, s); run; run = w.next(s), ++seg)
         for (int t = s.t0; t < s.t1; ++t, ++g) {
             const uint32_t st = g % kStages<D>;
@@ -360,13 +425,13 @@ __device__ void mma_one_role(SharedStorage<D>& sh, const Params& prm, const Plan
             tc_fence_after();
             const uint32_t vl = v_lo0 + st * kStageStep, kl = k_lo0 + st * kStageStep;
             if (t == s.t0) {
-                if (have_prev && !issue_pv(vl, prev_first, true, seg - 1)) return;
+                if (have_prev && !issue_pv(vl, prev_first, true, prev_masked, seg - 1)) return;
                 if (!mbar_wait(&sh.q_full[0], seg & 1, &sh.abort, prm.wait_ns)) return;
                 tc_fence_after();
                 issue_qk(kl);
             } else {
                 issue_qk(kl);
-                if (!issue_pv(vl, prev_first, false, seg)) return;
+                if (!issue_pv(vl, prev_first, false, prev_masked, seg)) return;
             }
             if (issuer) {
                 tc_commit(&sh.kv_empty[st]);
@@ -374,12 +439,13 @@ __device__ void mma_one_role(SharedStorage<D>& sh, const Params& prm, const Plan
             }
             have_prev = true;
             prev_first = t == s.t0;
+            prev_masked = t >= s.masked;
         }
     if (have_prev) {
         const uint32_t st = g % kStages<D>;
         if (!mbar_wait(&sh.kv_full[st], (g / kStages<D>) & 1, &sh.abort, prm.wait_ns)) return;
         tc_fence_after();
-        issue_pv(v_lo0 + st * kStageStep, prev_first, true, seg - 1);
+        issue_pv(v_lo0 + st * kStageStep, prev_first, true, prev_masked, seg - 1);
     }
 }
 
@@ -453,8 +519,37 @@ __device__ __forceinline__ float weights32(const uint32_t* sv, float a, float ad
     return s0 + s1;
 }
 
+// Where values that are not numbers were taken out of a run: in which of the 32 columns from `col` on one had been that a row sees, a bit each.  (By
+// reading the run's last tiles again: for a run that had any.)
 template <int D>
-__device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem, int t /*M tile*/)
+__device__ __forceinline__ uint32_t nan_columns(const Params& prm, const BlockParams& bp, const Segment& s, int r, uint64_t mask, int col)
+{
+    uint32_t bits = 0u;
+    const int T = prm.d.T, R = prm.d.T + prm.d.C, S = prm.d.S;
+    const size_t pitch = (size_t)prm.d.Hkv * D;
+#pragma unroll 1
+    for (int t = max(s.t0, s.masked); t < s.t1; ++t) {
+        const bool soft = t >= s.nkt;
+        const int page = soft ? 0 : __ldg(prm.map.block_table + (size_t)s.b * prm.map.max_pages + t);
+        if ((uint32_t)page >= (uint64_t)bp.n_pages) continue;
+        uint64_t lo, hi;
+        visible_bits(s, t, R, T, S, r, true, mask, lo, hi);
+        const uint8_t* v = (soft ? bp.v_soft : bp.v) + (size_t)page * kTileKeys * pitch + s.g * D + col;
+#pragma unroll 1
+        for (int key = 0; key < kTileKeys; ++key) {
+            if (!(((key < 64 ? lo : hi) >> (key & 63)) & 1ull)) continue;
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t nm = e4m3_nan4(__ldg(reinterpret_cast<const uint32_t*>(v + key * pitch) + k)) & 0x01010101u;
+                bits |= ((nm | nm >> 7 | nm >> 14 | nm >> 21) & 0xfu) << (4 * k);
+            }
+        }
+    }
+    return bits;
+}
+
+template <int D>
+__device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, uint32_t tmem, int t /*M tile*/)
 {
     const int lane_row = threadIdx.x & 127;                 // row of the M tile = TMEM lane
     const int warp_in_wg = (threadIdx.x >> 5) & 3;
@@ -558,11 +653,18 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Plan
             p_ptr = prm.partials + (size_t)s.part_slot * (partial_slot_bytes() / sizeof(float)) +
                     (size_t)(t * 128 + warp_in_wg * 32 + (lane >> 3)) * kPartD + 4 * (lane & 7);
         }
+        const bool nan = *reinterpret_cast<volatile int*>(&sh.nan_run[seg % 8]) == (int)seg + 1 && row_valid;
 #pragma unroll 1
         for (int q4 = 0; q4 < D / 32; ++q4) {
             uint32_t ov[32];
             tmem_ld32(o_addr + q4 * 32, ov);
             tc_wait_ld();
+            if (nan) {
+                const uint32_t bits = nan_columns<D>(prm, bp, s, r, mask, 32 * q4);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if ((bits >> j) & 1u) ov[j] = 0x7fffffffu;
+            }
 #pragma unroll
             for (int q = 0; q < 8; ++q)
                 xp[lane * 8 + (q ^ (lane & 7))] =
@@ -604,7 +706,7 @@ __device__ void softmax_role(SharedStorage<D>& sh, const Params& prm, const Plan
 // The softmax threads with one M tile: two warpgroups have the same rows and half of every tile's keys each, with a reference maximum, a sum and an
 // accumulator of its own; they meet once, at the end of a run.
 template <int D>
-__device__ void softmax_one_role(SharedStorage<D>& sh, const Params& prm, const PlanView& pv, uint32_t tmem, int half)
+__device__ void softmax_one_role(SharedStorage<D>& sh, const Params& prm, const BlockParams& bp, const PlanView& pv, uint32_t tmem, int half)
 {
     const int lane_row = threadIdx.x & 127, wq = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
@@ -716,12 +818,19 @@ __device__ void softmax_one_role(SharedStorage<D>& sh, const Params& prm, const 
         if (!mbar_wait(&sh.o_done[0], seg & 1, &sh.abort, prm.wait_ns)) return;
         tc_fence_after();
         constexpr int kChunks = D / 64;                      // of 32 columns; this half's warps write D / 2 columns
+        const bool nan = *reinterpret_cast<volatile int*>(&sh.nan_run[seg % 8]) == (int)seg + 1 && row_valid;
 #pragma unroll 1
         for (int q4 = kChunks * half; q4 < kChunks * half + kChunks; ++q4) {
             uint32_t u0[32], u1[32];
             tmem_ld32(tmem + lane_base + 256 + q4 * 32, u0);
             tmem_ld32(tmem + lane_base + 384 + q4 * 32, u1);
             tc_wait_ld();
+            if (nan) {
+                const uint32_t bits = nan_columns<D>(prm, bp, s, r, mask, 32 * q4);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if ((bits >> j) & 1u) u0[j] = 0x7fffffffu;
+            }
             auto sum = [&](int i) { return fmaf(__uint_as_float(u0[i]), f0, __uint_as_float(u1[i]) * f1); };
 #pragma unroll
             for (int q = 0; q < 8; ++q) xp[lane * 8 + (q ^ (lane & 7))] = make_float4(sum(4 * q), sum(4 * q + 1), sum(4 * q + 2), sum(4 * q + 3));
@@ -777,6 +886,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
             for (int h = 0; h < 2; ++h) mbar_init(&sh.p_one[t][h], 128);
         }
         mbar_init(&sh.o_read, 256);
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.scan_full[i], 1); mbar_init(&sh.scan_empty[i], 1); }
+        for (int i = 0; i < 8; ++i) sh.nan_run[i] = 0;
         mbar_init(&sh.met, 256);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -800,8 +911,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int t = warp >> 2;
-        if constexpr (kOne) softmax_one_role<D>(sh, prm, pv, tmem, t);
-        else if (t < prm.n_mt) softmax_role<D>(sh, prm, pv, tmem, t);
+        if constexpr (kOne) softmax_one_role<D>(sh, prm, bp, pv, tmem, t);
+        else if (t < prm.n_mt) softmax_role<D>(sh, prm, bp, pv, tmem, t);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         convert_role<D>(sh, prm);
@@ -815,7 +926,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_block_tc_kernel(const _
             tiles_role<D>(sh, prm, bp, pv, &k_map, &v_map);
         else if (warp == 14) {
             if ((threadIdx.x & 31) == 0) q_role<D>(sh, prm, pv, &q_map);
-        }
+        } else
+            scan_role<D>(sh, prm, bp, pv);
         __syncwarp();
     }
     // ---- teardown ----

@@ -47,6 +47,12 @@ __device__ __forceinline__ void e4m3_to_f32x4(uint32_t codes, float (&x)[4])
     f16x2_to_f32(hi, x[2], x[3]);
 }
 
+// Or-ed together for any number of words: bits of 0x80808080 are set where one of the codes is not a number (0x7f, 0xff).
+__device__ __forceinline__ uint32_t e4m3_nan_trace(uint32_t codes) { return (codes & 0x7f7f7f7fu) + 0x01010101u; }
+constexpr uint32_t kNanTrace = 0x80808080u;
+// 0xff in the place of every code that is not a number
+__device__ __forceinline__ uint32_t e4m3_nan4(uint32_t codes) { return __vcmpeq4(codes & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+
 // The smallest power of two 2^e, e >= -100, with amax <= 448 * 2^e (448 = 0.875 * 2^9), for a finite amax >= 0.  A power of two: encoding
 // an entry again for a block whose scale has grown then only drops bits below the smallest E4M3 step, it never rounds
 // a rounded value a second time, and scale times code is exact.

@@ -188,6 +188,48 @@ def test_pages_outside_the_pool_read_as_zeros_and_a_malformed_tree_as_a_status(g
         assert (np.abs(out[:2] - want[:2]) <= tol[:2]).all() and (np.abs(lse[:2] - want_lse[:2]) <= tol_lse[:2]).all()
 
 
+@pytest.mark.parametrize("kw", [dict(T=6, C=2, S=20, prefix=[250, 60, 126]), dict(T=6, C=2, S=0, D=64, Hq=4, prefix=[250, 60, 126]),
+                                dict(T=8, C=4, S=3, Hq=4, Hkv=2, prefix=[250, 60, 126]), dict(T=40, C=20, S=40, prefix=[250, 60, 126]),
+                                dict(B=40, T=40, C=20, S=5, prefix=(0, 300), Hkv=4, Hq=16), dict(B=40, T=40, C=20, S=5, prefix=(0, 300), Hkv=4, Hq=16, D=64)])
+def test_values_that_are_not_numbers_reach_the_rows_that_see_them_alone(gpu, kw):
+    """NaN codes in keys and values of tree slots and soft prompts, a column of a value each: exactly the rows that see them, exactly that column."""
+    case = Case(seed=51, **kw)
+    r = case.r
+    bad_v = np.zeros((case.B, case.T + case.C + case.S, case.Hkv, case.D), bool)
+    bad_k = np.zeros((case.B, case.T + case.C + case.S, case.Hkv), bool)
+    for b in range(case.B):
+        for _ in range(3):
+            j, h, d = r.randint(0, case.R), r.randint(0, case.Hkv), r.randint(0, case.D)
+            case.v.codes[case.v.slot(b, int(case.P[b]) + j), h, d] = r.choice([0x7f, 0xff])
+            bad_v[b, j, h, d] = True
+        if b % 2:
+            j, h = r.randint(case.R // 2, case.R), r.randint(0, case.Hkv)
+            case.k.codes[case.k.slot(b, int(case.P[b]) + j), h, 5] = 0x7f
+            bad_k[b, j, h] = True
+    if case.S:
+        case.v_soft[case.S - 1, 0, 7] = 0xff
+        bad_v[:, case.R + case.S - 1, 0, 7] = True
+    want = np.zeros((case.B, case.R, case.Hq, case.D), bool)
+    G = case.Hq // case.Hkv
+    for b in range(case.B):
+        see = br.visible(int(case.P[b]), case.T, case.C, case.S, case.parent[b], case.owner[b])[:, int(case.P[b]):]
+        for h in range(case.Hq):
+            want[b, :, h] = (see @ bad_v[b, :, h // G].astype(int) > 0) | (see @ bad_k[b, :, h // G].astype(int) > 0)[:, None]
+    d = case.device()
+    # numbers in their places: what the rows that do not see them, and their other columns, are
+    case.v.codes[(case.v.codes & 127) == 127] = 0
+    case.k.codes[(case.k.codes & 127) == 127] = 0
+    case.v_soft[(case.v_soft & 127) == 127] = 0
+    out, _, tol, _ = case.want()
+    for path in paths_of(gpu, case):
+        gpu.set_path(path)
+        got, lse, status = attend(gpu, case, d)
+        assert (status == 0).all()
+        assert np.array_equal(np.isnan(got), want), f"path {path}"
+        fine = ~want
+        assert (np.abs(got[fine] - out[fine]) <= tol[fine]).all(), f"path {path}"
+
+
 # ------------------------------------------------------------------------------------------------ writing
 def layers(case, n, seed):
     r = np.random.RandomState(seed)
