@@ -32,7 +32,8 @@ int check_pages(const confu_pages* p, int32_t n)
 {
     if (!p || n < 0 || !p->ref_count || !p->block_table) return CONFU_ERR_ARG;
     if (p->n_pages <= 0 || p->n_rows <= 0 || p->max_pages <= 0) return CONFU_ERR_SHAPE;
-    if (n > CONFU_MAX_PAGE_REQUESTS) return CONFU_ERR_UNSUPPORTED;
+    // (slots are counted in 32 bits)
+    if (n > CONFU_MAX_PAGE_REQUESTS || p->n_pages > INT32_MAX / kTileKeys || p->max_pages > INT32_MAX / kTileKeys) return CONFU_ERR_UNSUPPORTED;
     return misaligned(p->ref_count) || misaligned(p->block_table) ? CONFU_ERR_ALIGN : CONFU_OK;
 }
 
@@ -552,6 +553,7 @@ int confu_pages_copy(confu_ctx* ctx, const confu_dims* dims, int32_t n_layers, v
                      int32_t n_pages, int32_t n, const int32_t* src_pages, const int32_t* dst_pages, int32_t* status, void* stream)
 {
     if (!ctx || n < 0 || n_pages <= 0) return CONFU_ERR_ARG;
+    if (n_pages > INT32_MAX / kTileKeys) return CONFU_ERR_UNSUPPORTED;
     const int rc = check_page_pools(ctx, dims, n_layers, k_cache_layers, v_cache_layers);
     if (rc != CONFU_OK || n == 0) return rc;
     if (!src_pages || !dst_pages) return CONFU_ERR_ARG;

@@ -145,10 +145,11 @@ def test_pages(ctx):
         for bad in (pages(n=0), pages(rows=0), pages(width=-1)):
             assert call(bad) == SHAPE
         assert call(pages(ref=AT + 4)) == ALIGN
+        assert call(pages(n=(1 << 24))) == UNSUPPORTED and call(pages(width=1 << 24)) == UNSUPPORTED      # 2^31 slots
     for call in (fork, reserve, free):
         assert call(n=-1) == ARG and call(n=1025) == UNSUPPORTED and call(n=0) == 0
     assert reserve(rows=st) == ARG and free(rows=st) == ARG and fork(src=st) == ARG and copy(src=st) == ARG
-    assert fork(layers=-1) == ARG and fork(k=st) == ARG and copy(n=-1) == ARG and copy(n_pages=0) == ARG and copy(n=0) == 0
+    assert fork(layers=-1) == ARG and fork(k=st) == ARG and copy(n=-1) == ARG and copy(n_pages=0) == ARG and copy(n_pages=1 << 24) == UNSUPPORTED and copy(n=0) == 0
     assert fork(ws=st) == WORKSPACE and fork(ws_bytes=100) == WORKSPACE and fork(ws=C.c_void_p(AT + 8)) == ALIGN
     assert compact(used=st) == ARG and compact(ws_bytes=100) == WORKSPACE
     block = dims()
