@@ -153,6 +153,111 @@ def test_attention(gpu, name):
         assert np.array_equal(got[0], again[0]) and np.array_equal(got[1], again[1])
 
 
+# many stretches of several tiles for a CTA each: rings and barriers go round often
+RUNS = {
+    "one_token": dict(B=64, Hq=8, Hkv=8, T=1, C=0, S=0, prefix=(100, 900)),
+    "one_token_g4_d64": dict(B=48, Hq=16, Hkv=4, D=64, T=1, C=0, S=4, prefix=(100, 900), block=32),
+    "chain": dict(B=40, Hq=8, Hkv=4, T=9, C=2, S=4, prefix=(100, 900)),
+    "trees": dict(B=40, Hq=8, Hkv=4, T=40, C=10, S=4, prefix=(100, 700)),
+    "trees_two_tiles": dict(B=24, Hq=32, Hkv=8, T=40, C=10, S=4, prefix=(0, 500)),
+    "trees_d64": dict(B=40, Hq=8, Hkv=4, D=64, T=40, C=10, S=4, prefix=(100, 700)),
+    "thousands": dict(B=3001, Hq=2, Hkv=2, T=1, C=0, S=0, prefix=(0, 40)),
+    "heads_30": dict(B=5, Hq=30, Hkv=30, T=2, C=1, S=2, prefix=(0, 500)),
+    "heads_74": dict(B=5, Hq=74, Hkv=74, T=2, C=1, S=2, prefix=(0, 300)),
+    "heads_200": dict(B=2, Hq=200, Hkv=200, T=2, C=1, S=2, prefix=(0, 300)),
+}
+
+
+@pytest.mark.parametrize("name", RUNS)
+def test_attention_of_many_sequences(gpu, name):
+    case = Case(seed=350 + list(RUNS).index(name), **RUNS[name])
+    d = case.device()
+    for path in paths_of(gpu, case):
+        gpu.set_path(path)
+        got = attend(gpu, case, d)
+        compare(case, got, what=f"{name}, path {path}")
+        for _ in range(5):
+            again = attend(gpu, case, d)
+            assert np.array_equal(got[0], again[0]) and np.array_equal(got[1], again[1])
+
+
+@pytest.mark.parametrize("kw", [dict(T=3, C=1), dict(T=3, C=1, Hkv=1, Hq=4)])
+def test_a_plan_for_the_other_kernel_is_refused(gpu, kw):
+    """Nothing is written but the status."""
+    case = Case(seed=45, **kw)
+    d = case.device()
+    dims = case.dims()
+    gpu.ensure_ws(dims)
+    cb.confu_set_paging(gpu.ctx, d["table"], d["table"].shape[1])
+    cb.confu_set_kv_block_scales(gpu.ctx, d["ks"], d["vs"], d["ks_soft"], d["vs_soft"], case.block)
+    for built, launched in ((cb.ATTENTION_GENERIC, cb.ATTENTION_TENSOR), (cb.ATTENTION_TENSOR, cb.ATTENTION_GENERIC)):
+        gpu.set_path(built)
+        reg = []
+        plan = H.guarded(reg, (cb.confu_plan_bytes(gpu.ctx, dims),), torch.uint8)
+        out = H.guarded(reg, d["q"].shape, torch.bfloat16, 7.0)
+        lse = H.guarded(reg, (case.B, case.R, case.Hq), torch.float32, 7.0)
+        status = H.guarded(reg, (case.B,), torch.int32, 0)
+        cb.confu_tree_plan(gpu.ctx, dims, None, d["P"], d["parent"], d["owner"], plan, status)
+        gpu.set_path(launched)
+        cb.confu_tree_attention(gpu.ctx, dims, d["q"], d["k"], d["v"], case.n_pages * PAGE, None, d["P"], d["k_soft"], d["v_soft"], None, None, plan, out, lse,
+                                status)
+        torch.cuda.synchronize()
+        H.assert_guards(reg, "refused plan")
+        assert status.cpu().tolist() == [cb.ST_BAD_PLAN] * case.B
+        assert (out == 7.0).all() and (lse == 7.0).all()
+
+
+@pytest.mark.parametrize("T,C", [(3, 1), (30, 10)])
+def test_entries_behind_four_gigabytes(gpu, T, C):
+    """A pool of which the last pages alone are in use, past 2^32 bytes: append, attention, compaction and copies give what a small pool gives."""
+    Hkv, D = 8, 128
+    case = Case(Hq=8, Hkv=Hkv, T=T, C=C, prefix=[200, 60, 126], seed=47)
+    page_bytes = PAGE * Hkv * D
+    skip = 2 ** 32 // page_bytes + 3
+    n_pages = skip + case.n_pages
+    small, big = case.device(), case.device()
+    for n in ("k", "v"):
+        pool = torch.empty(n_pages * PAGE, Hkv, D, dtype=torch.uint8, device="cuda")
+        pool[skip * PAGE:] = big[n]
+        scales = torch.ones(n_pages, Hkv, PAGE // case.block, device="cuda")
+        scales[skip:] = big[n + "s"]
+        big[n], big[n + "s"] = pool, scales
+    big["table"] = torch.where(big["table"] >= 0, big["table"] + skip, big["table"])
+    rows = [torch.from_numpy(case.r.randn(case.B, case.R, Hkv, D).astype(np.float32)).bfloat16().cuda() for _ in range(2)]
+    a, path = paths(case)
+    dims = case.dims()
+    gpu.ensure_ws(dims)
+    results = []
+    for d, first, total in ((small, 0, case.n_pages), (big, skip, n_pages)):
+        ptrs = [torch.tensor([d[n].data_ptr()], dtype=torch.int64, device="cuda") for n in ("k", "v", "ks", "vs")]
+        cb.confu_set_paging(gpu.ctx, d["table"], d["table"].shape[1])
+        cb.confu_set_kv_block_scales(gpu.ctx, d["ks"], d["vs"], d["ks_soft"], d["vs_soft"], case.block)
+        cb.confu_set_kv_block_scale_layers(gpu.ctx, ptrs[2], ptrs[3], case.block)
+        cb.confu_kv_append(gpu.ctx, dims, rows[0], rows[1], d["k"], d["v"], None, d["P"])
+        outs = []
+        for kernel in paths_of(gpu, case):
+            gpu.set_path(kernel)
+            out = torch.zeros_like(d["q"])
+            status = torch.zeros(case.B, dtype=torch.int32, device="cuda")
+            cb.confu_tree_attention(gpu.ctx, dims, d["q"], d["k"], d["v"], total * PAGE, None, d["P"], d["k_soft"], d["v_soft"], d["parent"], d["owner"], None,
+                                    out, None, status)
+            torch.cuda.synchronize()
+            assert (status == 0).all()
+            outs.append(out)
+        gpu.set_path(cb.ATTENTION_AUTO)
+        new = torch.zeros(case.B, dtype=torch.int32, device="cuda")
+        cb.confu_kv_compact(gpu.ctx, dims, 1, ptrs[0], ptrs[1], None, d["P"], to_cuda(a), to_cuda(path), new, status)
+        used = sorted(set(case.table[case.table >= 0].tolist()))
+        pair = [torch.tensor([first + used[i]], dtype=torch.int32, device="cuda") for i in (0, -1)]
+        cb.confu_pages_copy(gpu.ctx, dims, 1, ptrs[0], ptrs[1], total, pair[0], pair[1], status[:1])
+        torch.cuda.synchronize()
+        assert (status == 0).all()
+        results.append(outs + [d["k"][first * PAGE:], d["v"][first * PAGE:], d["ks"][first:], d["vs"][first:]])
+    assert torch.isfinite(results[0][0].float()).all()
+    for x, y in zip(*results):
+        assert torch.equal(torch.nan_to_num(x.float()) if x.dtype == torch.float32 else x, torch.nan_to_num(y.float()) if y.dtype == torch.float32 else y)
+
+
 def test_attention_with_another_scale_and_rows_of_any_size(gpu):
     case = Case(seed=41, T=6, C=2)
     case.q[0, 0] = 0.0                                               # equal weights
