@@ -74,17 +74,45 @@ __device__ __forceinline__ uint2 encode8(const uint4& v, const Divisor& d)
     return make_uint2(e4m3_pack4(x[0], x[1], x[2], x[3]), e4m3_pack4(x[4], x[5], x[6], x[7]));
 }
 
-// four codes of a block with scale `was` -> codes for another scale
-__device__ __forceinline__ uint32_t recode4(uint32_t codes, float was, const Divisor& now)
-{
-    float x[4];
-    e4m3_to_f32x4(codes, x);
-    return e4m3_pack4(now.of(x[0] * was), now.of(x[1] * was), now.of(x[2] * was), now.of(x[3] * was));
-}
-__device__ __forceinline__ uint4 recode16(const uint4& v, float was, const Divisor& now)
-{
-    return make_uint4(recode4(v.x, was, now), recode4(v.y, was, now), recode4(v.z, was, now), recode4(v.w, was, now));
-}
+// Codes of a block with scale `was` -> codes for another scale.  Where both are powers of two, was / now = 2^k is one, and the product is made in f16,
+// two codes at a time: exact down to 2^-24 (a code has four bits, its lowest 2^-9 at least, and what lies below 2^-20 is a zero code
+// either way) and, with k <= 15, no larger than 448 * 2^15 only in numbers that saturate, to 448, either way.
+struct Recode {
+    Divisor by;
+    float was;
+    uint32_t ratio;                                  // f16, twice; 0xffffffff: a power of two is missing
+    __device__ __forceinline__ Recode(float from, float to) : by(to), was(from)
+    {
+        const Divisor d(from);
+        const int k = (int)(__float_as_uint(from) >> 23) - (int)(__float_as_uint(to) >> 23);
+        const uint32_t h = k < -24 ? 0u : k < -14 ? 1u << (k + 24) : (uint32_t)(k + 15) << 10;
+        ratio = by.product && d.product && k <= 15 ? h * 0x10001u : 0xffffffffu;
+    }
+    __device__ __forceinline__ uint32_t four(uint32_t codes) const
+    {
+        uint32_t lo, hi, r;
+        e4m3_to_f16x4(codes, lo, hi);
+        asm("{\n\t.reg .b16 a, b;\n\t"
+            "mul.rn.f16x2 %1, %1, %3;\n\t"
+            "mul.rn.f16x2 %2, %2, %3;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\t"
+            "mov.b32 %0, {a, b};\n\t}"
+            : "=&r"(r), "+r"(lo), "+r"(hi)
+            : "r"(ratio));
+        return r;
+    }
+    __device__ __noinline__ uint32_t any_four(uint32_t codes) const
+    {
+        float x[4];
+        e4m3_to_f32x4(codes, x);
+        return e4m3_pack4(by.of(x[0] * was), by.of(x[1] * was), by.of(x[2] * was), by.of(x[3] * was));
+    }
+    __device__ __forceinline__ uint4 of(const uint4& v) const
+    {
+        return ratio != 0xffffffffu ? make_uint4(four(v.x), four(v.y), four(v.z), four(v.w)) : make_uint4(any_four(v.x), any_four(v.y), any_four(v.z), any_four(v.w));
+    }
+};
 
 // Where block `jb` of sequence b lies: its first slot in the pool and its place in the scales.  A negative page id has none.
 struct BlockAt {
@@ -151,11 +179,14 @@ __global__ void __launch_bounds__(kAppendThreads<D, kRowsMost>) append_block_ker
     const float now = fmaxf(was, e4m3_block_scale(m));
     if (threadIdx.x == 0) *scale = now;
     const Divisor by(now);
-    if (kept > 0 && now > was)
+    if (kept > 0 && now > was) {
+        const Recode again(was, now);
+#pragma unroll 4
         for (int u = threadIdx.x; u < kept * (D / 16); u += kThreads) {
             uint4* p = reinterpret_cast<uint4*>(codes + (u / (D / 16)) * pitch + (u % (D / 16)) * 16);
-            *p = recode16(*p, was, by);
+            *p = again.of(*p);
         }
+    }
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
         const int r = row0 + i * kRows;
@@ -258,10 +289,10 @@ __global__ void __launch_bounds__(kCompactThreads) compact_block_kernel(int T, i
     // what stays in the block that the root is in
     const int kept = off0 + 1 - jb0 * block;
     if (kept > 0 && now[0] > was[0] && there(jb0 * block)) {
-        const Divisor by(now[0]);
+        const Recode again(was[0], now[0]);
         for (int u = lane; u < kept * kPerRow; u += 32) {
             uint4* p = reinterpret_cast<uint4*>(entry(jb0 * block + u / kPerRow) + (u % kPerRow) * 16);
-            *p = recode16(*p, was[0], by);
+            *p = again.of(*p);
         }
     }
     for (int k0 = 1; k0 <= a; k0 += kBatch * kRows) {
@@ -275,7 +306,7 @@ __global__ void __launch_bounds__(kCompactThreads) compact_block_kernel(int T, i
             if (!(from[i] > 0.f)) continue;
             const int s = off0 + k0 + row0 + i * kRows, j = s / block - jb0;
             const float s_to = j == 0 ? now[0] : j == 1 ? now[1] : now[2];
-            if (there(s)) *reinterpret_cast<uint4*>(entry(s) + col * 16) = from[i] == s_to ? v[i] : recode16(v[i], from[i], Divisor(s_to));
+            if (there(s)) *reinterpret_cast<uint4*>(entry(s) + col * 16) = from[i] == s_to ? v[i] : Recode(from[i], s_to).of(v[i]);
         }
     }
     __syncwarp();

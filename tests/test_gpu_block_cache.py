@@ -381,6 +381,31 @@ def test_append(gpu, name, size):
         same(d[n], want, n)
 
 
+@pytest.mark.parametrize("was", [1.0, 0.75])
+def test_every_code_is_encoded_again_for_every_larger_scale(gpu, was):
+    """All codes as prefix entries of a block whose scale grows 2^0 .. 2^39 times: each is the nearest code of its value."""
+    n = 40
+    case = Case(B=n, Hq=1, Hkv=1, T=1, C=0, S=0, prefix=[2] * n, block=32, rows_in=False, seed=63)
+    rows = torch.zeros(n, 1, 1, 128, dtype=torch.bfloat16)
+    for b in range(n):
+        for c in (case.k, case.v):
+            c.scale(b, 0)[:] = was
+            c.codes[c.slot(b, 0), 0], c.codes[c.slot(b, 1), 0] = np.arange(128), np.arange(128, 256)
+        rows[b] = 448.0 * 2.0 ** b
+    d = case.device()
+    cb.confu_set_paging(gpu.ctx, d["table"], d["table"].shape[1])
+    cb.confu_set_kv_block_scales(gpu.ctx, d["ks"], d["vs"], None, None, case.block)
+    cb.confu_kv_append(gpu.ctx, case.dims(), rows.cuda(), rows.cuda(), d["k"], d["v"], None, d["P"])
+    torch.cuda.synchronize()
+    for b in range(n):
+        case.k.append(b, 2, rows[b].double().numpy())
+        assert case.k.scale(b, 0)[0] == max(was, 2.0 ** b)
+    same(d["ks"], case.k.scales, "scales")
+    got, want = d["k"].cpu().numpy(), case.k.codes
+    nan = (want & 127) == 127
+    assert np.array_equal((got & 127) == 127, nan) and np.array_equal(got[~nan], want[~nan])
+
+
 def test_append_of_rows_that_are_not_numbers(gpu):
     case = Case(B=2, T=5, C=0, prefix=[40, 0], block=32, rows_in=False, seed=61)
     rows = torch.from_numpy(case.r.randn(2, 5, 2, 128).astype(np.float32)).bfloat16()
