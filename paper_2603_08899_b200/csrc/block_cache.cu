@@ -41,7 +41,7 @@ __device__ __noinline__ float finite_amax8(uint4 v)
 }
 
 // What an entry is divided by.  By a power of two, which every scale is that was found here, that is a product: the same number, and eight
-// divisions less per 16 bytes of a row.  (With warps per head in the compaction: 32 sequences, 120 rows, 16 layers and the compaction 292 -> 155 us.)
+// divisions less per 16 bytes of a row.  (With warps per head in the compaction: 32 sequences, 120 rows, 16 layers and the compaction 292 -> 155 us, before CTAs took two blocks.)
 struct Divisor {
     float s, inv;
     bool product;
@@ -114,25 +114,26 @@ struct Recode {
     }
 };
 
-// Where block `jb` of sequence b lies: its first slot in the pool and its place in the scales.  A negative page id has none.
+// Where block `jb` of sequence b lies: its first slot in the pool and its place in the scales.  A negative page id has none.  (A block is 2^sh slots.)
 struct BlockAt {
     int64_t slot, scale;
     bool ok;
 };
-__device__ __forceinline__ BlockAt block_at(const SlotMap& map, int b, int64_t jb, int block, int Hkv, int g)
+__device__ __forceinline__ BlockAt block_at(const SlotMap& map, int b, int64_t jb, int sh, int Hkv, int g)
 {
-    const int64_t s = jb * block;
+    const int64_t s = jb << sh;
     const int page = map.block_table[(size_t)b * map.max_pages + (s >> 7)];
-    const int sub = (int)(s & (kTileKeys - 1)) / block, nb = kTileKeys / block;
-    return {(int64_t)page * kTileKeys + (s & (kTileKeys - 1)), ((int64_t)page * Hkv + g) * nb + sub, page >= 0};
+    const int in_page = (int)(s & (kTileKeys - 1));
+    return {(int64_t)page * kTileKeys + in_page, (((int64_t)page * Hkv + g) << (7 - sh)) + (in_page >> sh), page >= 0};
 }
 
-// CTA (sequence, kv head, K or V; block of slots): its rows' maximum, the scale, the codes.  As many threads as hold the rows that a block can get
-// (16, 32, 64 or 128: the block's slots or the step's rows) in four pieces each, eight where that would be
-// more than 256 (32 sequences, 120 rows, block 128: 155 us with 256, 197 with 512).
+// CTA (sequence, kv head, K or V): its rows' maxima, the scales, the codes.  With kTwo all of the step's rows, which lie in two blocks at most; else
+// the rows of one block (blockIdx.y).  As many threads as hold the rows (16, 32, 64 or 128) in four pieces each, eight where that would be
+// more than 256.  32 sequences, 120 rows, block 128, 16 layers and the compaction: 135 us, 158 with a CTA per block, which has pieces for 128 rows
+// and half of them to do.  (By 512 threads of four pieces, a CTA per block: 197.)
 template <int D, int kRowsMost> constexpr int kAppendThreads = kRowsMost * (D / 8) / 4 > 256 ? 256 : kRowsMost * (D / 8) / 4;
-template <int D, int kRowsMost>
-__global__ void __launch_bounds__(kAppendThreads<D, kRowsMost>) append_block_kernel(int R, int Hkv, int block, const __nv_bfloat16* __restrict__ k_rows,
+template <int D, int kRowsMost, bool kTwo>
+__global__ void __launch_bounds__(kAppendThreads<D, kRowsMost>) append_block_kernel(int R, int Hkv, int sh, const __nv_bfloat16* __restrict__ k_rows,
                                                                 const __nv_bfloat16* __restrict__ v_rows, uint8_t* k_cache, uint8_t* v_cache,
                                                                 float* k_scale, float* v_scale, const SlotMap map,
                                                                 const int32_t* __restrict__ prefix_len)
@@ -140,57 +141,80 @@ __global__ void __launch_bounds__(kAppendThreads<D, kRowsMost>) append_block_ker
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int kThreads = kAppendThreads<D, kRowsMost>, kPerRow = D / 8, kRows = kThreads / kPerRow, kMost = kRowsMost / kRows;   // units of eight entries
-    __shared__ float slots[kThreads / 32];
+    __shared__ float slots[2][kThreads / 32];
     const int kv = blockIdx.x & 1, g = (blockIdx.x >> 1) % Hkv, b = (blockIdx.x >> 1) / Hkv;
-    const int64_t P = prefix_len[b], jb = P / block + blockIdx.y;
-    const int64_t first = max(P, jb * block), end = min(P + R, (jb + 1) * block);
+    const int64_t P = prefix_len[b], jb = (P >> sh) + (kTwo ? 0 : (int)blockIdx.y);
+    const int64_t first = max(P, jb << sh), end = kTwo ? P + R : min(P + R, (jb + 1) << sh);
     if (first >= end) return;
     const __nv_bfloat16* rows = (kv ? v_rows : k_rows) + (((size_t)b * R + (size_t)(first - P)) * Hkv + g) * D;
-    const int n = (int)(end - first), kept = (int)(first - jb * block);
+    const int n = (int)(end - first), kept = (int)(first - (jb << sh)), split = kTwo ? min(n, (1 << sh) - kept) : n;       // rows of the first block
     const int row0 = threadIdx.x / kPerRow, col = threadIdx.x % kPerRow;
-    const size_t pitch = (size_t)Hkv * D;
+    const uint32_t pitch = (uint32_t)Hkv * D;
     uint4 v[kMost];
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
         const int r = row0 + i * kRows;
-        v[i] = r < n ? __ldg(reinterpret_cast<const uint4*>(rows + r * pitch + col * 8)) : make_uint4(0u, 0u, 0u, 0u);
+        v[i] = r < n ? __ldg(reinterpret_cast<const uint4*>(rows + (size_t)(r * pitch) + col * 8)) : make_uint4(0u, 0u, 0u, 0u);
     }
-    const BlockAt at = block_at(map, b, jb, block, Hkv, g);
-    if (!at.ok) return;
-    float* scale = (kv ? v_scale : k_scale) + at.scale;
-    uint8_t* codes = (kv ? v_cache : k_cache) + (at.slot * Hkv + g) * D;       // of the block's first slot; a slot is Hkv * D further on
-    const float was = kept > 0 ? *scale : 0.f;
-    uint32_t m2 = 0u;
+    const BlockAt at = block_at(map, b, jb, sh, Hkv, g);
+    BlockAt at1 = {0, 0, false};
+    if (kTwo && split < n) at1 = block_at(map, b, jb + 1, sh, Hkv, g);
+    if (!kTwo && !at.ok) return;
+    float* scales = kv ? v_scale : k_scale;
+    uint8_t* pool = (kv ? v_cache : k_cache) + (size_t)g * D;
+    const float was = at.ok && kept > 0 ? scales[at.scale] : 0.f;
+    uint32_t m2[2] = {0u, 0u};
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) m2 = max_bf16x2(m2, amax8(v[i]));
-    float m = larger_half(m2);
-    if (m == INFINITY) {
-        m = 0.f;
-        for (int i = 0; i < kMost; ++i) m = fmaxf(m, finite_amax8(v[i]));
+    for (int i = 0; i < kMost; ++i) {
+        const uint32_t x = amax8(v[i]);
+        const bool second = kTwo && row0 + i * kRows >= split;
+        m2[0] = max_bf16x2(m2[0], second ? 0u : x);
+        if (kTwo) m2[1] = max_bf16x2(m2[1], second ? x : 0u);
     }
-    m = warp_max(m);
-    if constexpr (kThreads > 32) {
-        if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = m;
-        __syncthreads();                             // (the old scale has been read by now, too)
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, slots[i]);
-    } else
-        __syncwarp();
-    const float now = fmaxf(was, e4m3_block_scale(m));
-    if (threadIdx.x == 0) *scale = now;
-    const Divisor by(now);
-    if (kept > 0 && now > was) {
-        const Recode again(was, now);
-#pragma unroll 4
-        for (int u = threadIdx.x; u < kept * (D / 16); u += kThreads) {
-            uint4* p = reinterpret_cast<uint4*>(codes + (u / (D / 16)) * pitch + (u % (D / 16)) * 16);
-            *p = again.of(*p);
+    float m[2] = {larger_half(m2[0]), larger_half(m2[1])};
+    if (m[0] == INFINITY || m[1] == INFINITY) {
+        m[0] = m[1] = 0.f;
+        for (int i = 0; i < kMost; ++i) {
+            const float x = finite_amax8(v[i]);
+            if (kTwo && row0 + i * kRows >= split) m[1] = fmaxf(m[1], x);
+            else m[0] = fmaxf(m[0], x);
         }
     }
 #pragma unroll
+    for (int j = 0; j < (kTwo ? 2 : 1); ++j) m[j] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m[j])));      // (not negative: ordered like their bits)
+    if constexpr (kThreads > 32) {
+        if ((threadIdx.x & 31) == 0) {
+            slots[0][threadIdx.x >> 5] = m[0];
+            if (kTwo) slots[1][threadIdx.x >> 5] = m[1];
+        }
+        __syncthreads();                             // (the old scale has been read by now, too)
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i) {
+            m[0] = fmaxf(m[0], slots[0][i]);
+            if (kTwo) m[1] = fmaxf(m[1], slots[1][i]);
+        }
+    } else
+        __syncwarp();
+    const float now = fmaxf(was, e4m3_block_scale(m[0])), now1 = kTwo ? e4m3_block_scale(m[1]) : now;
+    if (threadIdx.x == 0 && at.ok) scales[at.scale] = now;
+    if (kTwo && threadIdx.x == 0 && at1.ok) scales[at1.scale] = now1;
+    uint8_t* codes = pool + at.slot * pitch;
+    if (at.ok && kept > 0 && now > was) {
+        const Recode again(was, now);
+#pragma unroll 4
+        for (int u = threadIdx.x; u < kept * (D / 16); u += kThreads) {
+            uint4* p = reinterpret_cast<uint4*>(codes + (size_t)(u / (D / 16) * pitch) + (u % (D / 16)) * 16);
+            *p = again.of(*p);
+        }
+    }
+    const Divisor by(now), by1(now1);
+    codes += (size_t)(kept * pitch) + col * 8;
+    uint8_t* codes1 = pool + (at1.slot - split) * (int64_t)pitch + col * 8;
+#pragma unroll
     for (int i = 0; i < kMost; ++i) {
         const int r = row0 + i * kRows;
-        if (r < n) *reinterpret_cast<uint2*>(codes + (kept + r) * pitch + col * 8) = encode8(v[i], by);
+        const bool second = kTwo && r >= split;
+        if (r < n && (second ? at1.ok : at.ok)) *reinterpret_cast<uint2*>((second ? codes1 : codes) + (size_t)(r * pitch)) = encode8(v[i], second ? by1 : by);
     }
 }
 
@@ -321,14 +345,19 @@ cudaError_t launch_append_block(const Ctx* ctx, const confu_dims& d, const void*
                                 void* v_cache, const SlotMap& map, const int32_t* prefix_len, cudaStream_t st)
 {
     const int R = d.T + d.C;
-    // (as many blocks as R slots can touch, wherever the first of them lies)
-    const dim3 grid((unsigned)(2 * d.B * d.Hkv), (unsigned)((R + ctx->block - 2) / ctx->block + 1));
-    const int most = R < ctx->block ? R : ctx->block;
-    auto kernel = d.D == 64 ? (most <= 16 ? append_block_kernel<64, 16> : most <= 32 ? append_block_kernel<64, 32> : most <= 64 ? append_block_kernel<64, 64> : append_block_kernel<64, 128>)
-                            : (most <= 16 ? append_block_kernel<128, 16> : most <= 32 ? append_block_kernel<128, 32> : most <= 64 ? append_block_kernel<128, 64> : append_block_kernel<128, 128>);
-    const int rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128, threads = rows * (d.D / 8) / 4;
-    return launch_pdl(kernel, grid, dim3((unsigned)(threads > 256 ? 256 : threads)), st, R, (int)d.Hkv, ctx->block, (const __nv_bfloat16*)k_rows, (const __nv_bfloat16*)v_rows,
-                      (uint8_t*)k_cache, (uint8_t*)v_cache, ctx->k_block_scale, ctx->v_block_scale, map, prefix_len);
+    // as many blocks as R slots can touch, wherever the first of them lies; two at most are one CTA's
+    const int blocks = (R + ctx->block - 2) / ctx->block + 1, sh = ctx->block == 128 ? 7 : ctx->block == 64 ? 6 : 5;
+    const bool two = blocks <= 2;
+    const dim3 grid((unsigned)(2 * d.B * d.Hkv), (unsigned)(two ? 1 : blocks));
+    auto launch = [&](auto kernel, int threads) {
+        return launch_pdl(kernel, grid, dim3((unsigned)threads), st, R, (int)d.Hkv, sh, (const __nv_bfloat16*)k_rows, (const __nv_bfloat16*)v_rows,
+                          (uint8_t*)k_cache, (uint8_t*)v_cache, ctx->k_block_scale, ctx->v_block_scale, map, prefix_len);
+    };
+#define APPEND(D, ROWS, TWO) launch(append_block_kernel<D, ROWS, TWO>, kAppendThreads<D, ROWS>)
+#define APPEND_OF(D) (!two ? (sh == 5 ? APPEND(D, 32, false) : APPEND(D, 64, false)) : R <= 16 ? APPEND(D, 16, true) : R <= 32 ? APPEND(D, 32, true) : R <= 64 ? APPEND(D, 64, true) : APPEND(D, 128, true))
+    return d.D == 64 ? APPEND_OF(64) : APPEND_OF(128);
+#undef APPEND_OF
+#undef APPEND
 }
 
 cudaError_t launch_compact_block(const Ctx* ctx, const confu_dims& d, int n_layers, void* const* k_layers, void* const* v_layers,
