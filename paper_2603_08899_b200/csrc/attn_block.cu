@@ -12,7 +12,7 @@
 // bytes are on their way.  One CTA per SM walks its share of key tiles in chunks of 32 keys, which 12 warps (8 for more than 16 rows) take in turn.
 // Every warp has a ring of two chunks of its own (K and V codes, 8 KB at D = 128); lanes of three warps keep them filled by TMA, across the ends of
 // runs, another warp lays out the next run's Q.  (Codes loaded straight into the registers that the products read, 8 KB a warp
-// under way: 64 sequences of 100..8192, one row, 203 us a layer at 2.8 TB/s, the warps waiting for their loads half of the time.)
+// under way: 64 sequences of 100..8192, one row, 203 us a layer at 2.8 TB/s, the warps waiting for their loads half of the time; now 108 at 5.1.)
 //   S = Q K^T    a lane's fragment of K^T is 16 contiguous bytes of a key (the head dims of a product's 16 steps are whatever
 //                bytes the lane has; Q's fragments are laid out in shared memory to match)
 //   O += P V     keys in pairs: a lane has the same 16 columns of two neighbouring keys, byte permutes pair them up
@@ -20,7 +20,7 @@
 // kernel (attn_tc.cu).  mma.sync and not tcgen05: 16 rows fill its M, an eighth of a tcgen05 tile, and fragments need no second trip through
 // shared memory as f16.
 //
-// Keys past the sequence's last slot are masked and their V codes read as 0; page ids outside the pool are not followed and read as zeros.
+// Keys past the sequence's last slot are masked, and their V codes that are not numbers taken out; page ids outside the pool are not followed and read as zeros.
 // Every wait on a barrier is bounded; a warp whose wait ran out goes on without computing, so that the others find it at the barriers, and
 // CONFU_ST_TIMEOUT is reported.
 #include "e4m3.cuh"
@@ -303,8 +303,8 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
             if (ok) {
                 const uint8_t *k_tile = sh.kv[warp][at.slot][0], *v_tile = sh.kv[warp][at.slot][1];
                 const float4 scale = sh.scales[warp][at.slot];
-                // A value that is not a number must not reach the rows that do not see its key, and 0 times it would.  Where not every row sees every key
-                // such codes are taken out; whose NaN they are is found out at the end of the run.
+                // A value that is not a number must not reach the rows that do not see its key, and 0 times it would.  Where not every row sees every key,
+                // which is also where the last slot is, such codes are taken out; whose NaN they are is found out at the end of the run.
                 if (t >= s.masked) {
                     uint4* piece = reinterpret_cast<uint4*>(sh.kv[warp][at.slot][1]) + lane;
                     uint32_t trace = 0u;
@@ -314,10 +314,12 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
                         trace |= e4m3_nan_trace(c.x) | e4m3_nan_trace(c.y) | e4m3_nan_trace(c.z) | e4m3_nan_trace(c.w);
                     }
                     if (__any_sync(0xffffffffu, (trace & kNanTrace) != 0u)) {
-                        sh.nan_run[seg & 1] = (int)seg + 1;
+                        // (behind the last slot they are nobody's)
 #pragma unroll 1
                         for (int k = 0; k < Sh::kCodes / 512; ++k) {
                             const uint4 c = piece[32 * k];
+                            const uint32_t any = e4m3_nan4(c.x) | e4m3_nan4(c.y) | e4m3_nan4(c.z) | e4m3_nan4(c.w);
+                            if (any && (32 * k + lane) * 16 / D < left) sh.nan_run[seg & 1] = (int)seg + 1;
                             piece[32 * k] = make_uint4(c.x & ~e4m3_nan4(c.x), c.y & ~e4m3_nan4(c.y), c.z & ~e4m3_nan4(c.z), c.w & ~e4m3_nan4(c.w));
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the slot is filled by copies again)
@@ -429,14 +431,6 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
                                 vw[u][o][0] = v.x; vw[u][o][1] = v.y;
                             }
                         }
-                    if (left < kChunk)
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int o = 0; o < 2; ++o)
-                                if (8 * (2 * h + u) + 2 * x + o >= left)
-#pragma unroll
-                                    for (int k = 0; k < D / 32; ++k) vw[u][o][k] = 0u;
 #pragma unroll
                     for (int k = 0; k < D / 32; ++k) {       // four columns of a lane
                         uint32_t b0[4], b1[4];
