@@ -139,7 +139,7 @@ int confu_set_paging(confu_ctx* ctx, const int32_t* block_table, int32_t max_pag
  *                             for (status CONFU_ST_BAD_PLAN otherwise), as confu_attention_path names it.  For small
  *                             batches _AUTO takes a form of its own of _TENSOR, _TENSOR_NARROW (one
  *                             M tile of query rows per CTA), which cannot be set.  For CONFU_FP8_BLOCK _GENERIC
- *                             is the kernel for few rows (mma.sync, (T + C) * Hq/Hkv <= 32), _TENSOR takes every supported shape.
+ *                             is the kernel for few rows (mma.sync, (T + C) * Hq/Hkv <= 16, with D = 64 <= 32), _TENSOR takes every supported shape.
  *   CONFU_OPT_WAIT_LIMIT_NS   wall-clock limit of every wait on a barrier inside the tensor-core
  *                             kernels (default 2 s; 1 us .. 10 s).  A wait that runs out makes the
  *                             kernel release what it holds and report CONFU_ST_TIMEOUT.

@@ -8,7 +8,7 @@
 // an f16 number, and q, times the power of two that brings a row's largest magnitude into [1, 2), is one but for what is smaller than
 // 2^-17 of it: nothing else is rounded.
 //
-// Up to 32 rows (query rows x heads of a kv head): reading the cache binds, 2 D bytes a key, and what counts is how many
+// Up to 16 rows (query rows x heads of a kv head), 32 at D = 64: reading the cache binds, 2 D bytes a key, and what counts is how many
 // bytes are on their way.  One CTA per SM walks its share of key tiles in chunks of 32 keys, which 12 warps (8 for more than 16 rows) take in turn.
 // Every warp has a ring of two chunks of its own (K and V codes, 8 KB at D = 128); lanes of three warps keep them filled by TMA, across the ends of
 // runs, another warp lays out the next run's Q.  (Codes loaded straight into the registers that the products read, 8 KB a warp
@@ -619,8 +619,11 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const Params& prm, const BlockP
 }  // namespace blk
 }  // namespace tc
 
-// rows x heads of a kv head: two M tiles of 16 at most
-bool block_register_supported(const confu_dims& d) { return (d.T + d.C) * (d.Hq / d.Hkv) <= 32; }
+// Rows x heads of a kv head: one M tile of 16, two at D = 64, whose fragments are half as many.  From there on the tcgen05 kernel is faster, whose time
+// hardly depends on the rows (us, graph; this kernel / that one; one sequence of 4096 x 4 layers, 16 of 500..4000 x 2, 64 of 100..4000 x 2;
+// 8 kv heads).  D = 128: 4 rows 45 / 64, 51 / 91, 132 / 248; 16 rows 66 / 66, 82 / 92, 171 / 250; 20 rows, with two M tiles, 70 / 66, 95 / 94,
+// 249 / 251; 32 rows 78 / 66, 107 / 95, 267 / 253.  D = 64: 4 rows 39 / 53, 39 / 70; 32 rows 53 / 53, 61 / 70.
+bool block_register_supported(const confu_dims& d) { return (d.T + d.C) * (d.Hq / d.Hkv) <= (d.D == 64 ? 32 : 16); }
 
 // Whether the CTAs of a share are one per kv head: the rows of a slot's heads are neighbours in memory, and read at the same time they come from
 // DRAM as whole lines (the same loads without arithmetic: 4.8 TB/s head after head, 5.4 side by side).  Not where the heads would leave
@@ -663,8 +666,8 @@ cudaError_t launch_attention_block(const Ctx* ctx, const confu_dims& d, const vo
     bp.block = ctx->block;
     const int units = ctx->sm_count;
     cudaError_t e;
-    if ((d.T + d.C) * prm.G <= 16) e = d.D == 64 ? blk::launch<64, 1, 12>(maps, prm, bp, units, st) : blk::launch<128, 1, 12>(maps, prm, bp, units, st);
-    else e = d.D == 64 ? blk::launch<64, 2, 8>(maps, prm, bp, units, st) : blk::launch<128, 2, 8>(maps, prm, bp, units, st);
+    if (d.D == 128) e = blk::launch<128, 1, 12>(maps, prm, bp, units, st);
+    else e = (d.T + d.C) * prm.G <= 16 ? blk::launch<64, 1, 12>(maps, prm, bp, units, st) : blk::launch<64, 2, 8>(maps, prm, bp, units, st);
     if (e != cudaSuccess) return e;
     return launch_combine(prm, ctx->sm_count, st);
 }

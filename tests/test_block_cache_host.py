@@ -81,12 +81,13 @@ def test_dims_and_paths(ctx):
         assert cb.lib().confu_plan_bytes(C.byref(ctx), C.byref(dims(**kw))) > 0
     ctx.attention_path = cb.ATTENTION_TENSOR_PAIR
     assert path() == UNSUPPORTED
-    # 32 rows x heads of a kv head, 36 (one M tile), 256 of few and of many (sequence, kv head) pairs
-    few, one, whole, batch = dict(T=8, Cn=0), dict(T=9, Cn=0), dict(T=60, Cn=4), dict(T=60, Cn=4, B=100)
+    # 16 rows x heads of a kv head (32 at head dim 64), 20 (one M tile), 256 of few and of many (sequence, kv head) pairs
+    few, one, whole, batch = dict(T=4, Cn=0), dict(T=5, Cn=0), dict(T=60, Cn=4), dict(T=60, Cn=4, B=100)
     G, N, T = cb.ATTENTION_GENERIC, cb.ATTENTION_TENSOR_NARROW, cb.ATTENTION_TENSOR
     for option, want in ((cb.ATTENTION_AUTO, (G, N, N, T)), (cb.ATTENTION_GENERIC, (G,) + 3 * (UNSUPPORTED,)), (cb.ATTENTION_TENSOR, (N, N, N, T))):
         ctx.attention_path = option
         assert tuple(path(**kw) for kw in (few, one, whole, batch)) == want
+        assert tuple(path(D=64, **kw) for kw in (dict(T=8, Cn=0), dict(T=9, Cn=0), whole, batch)) == want
     ctx.attention_path, ctx.sm_count = cb.ATTENTION_AUTO, 1          # a share is walked by a CTA per group of query rows
     assert path(T=64, Cn=64) == UNSUPPORTED and path(**whole) == T and path(**one) == N
 

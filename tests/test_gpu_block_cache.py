@@ -77,7 +77,7 @@ def gpu():
 
 def paths_of(gpu, case):
     """The kernels that take these sizes."""
-    return [cb.ATTENTION_AUTO, cb.ATTENTION_TENSOR] + ([cb.ATTENTION_GENERIC] if case.R * case.Hq // case.Hkv <= 32 else [])
+    return [cb.ATTENTION_AUTO, cb.ATTENTION_TENSOR] + ([cb.ATTENTION_GENERIC] if case.R * case.Hq // case.Hkv <= (32 if case.D == 64 else 16) else [])
 
 
 def attend(gpu, case, d, use_plan=True, sm_scale=0.0, stream=None):
@@ -138,6 +138,9 @@ ATTEND = {
     "scales_apart_one_token": dict(T=1, C=0, S=0, wide=12, block=32, prefix=(200, 700)),
     "scales_not_powers_of_two": dict(odd_scales=True, block=32),
     "many_sequences": dict(B=40, Hq=4, Hkv=2, T=2, C=1, S=2, prefix=(0, 260)),
+    "rows_28_d64": dict(D=64, T=5, C=2),
+    "g32_d64": dict(B=2, D=64, Hq=32, Hkv=1, T=1, C=0, block=32),
+    "rows_16": dict(T=3, C=1),
 }
 
 
@@ -162,6 +165,8 @@ RUNS = {
     "trees_two_tiles": dict(B=24, Hq=32, Hkv=8, T=40, C=10, S=4, prefix=(0, 500)),
     "trees_d64": dict(B=40, Hq=8, Hkv=4, D=64, T=40, C=10, S=4, prefix=(100, 700)),
     "thousands": dict(B=3001, Hq=2, Hkv=2, T=1, C=0, S=0, prefix=(0, 40)),
+    "chain_d64": dict(B=40, Hq=8, Hkv=4, D=64, T=9, C=2, S=4, prefix=(100, 900)),
+    "chain_16_rows": dict(B=40, Hq=8, Hkv=4, T=6, C=2, S=4, prefix=(100, 900)),
     "heads_30": dict(B=5, Hq=30, Hkv=30, T=2, C=1, S=2, prefix=(0, 500)),
     "heads_74": dict(B=5, Hq=74, Hkv=74, T=2, C=1, S=2, prefix=(0, 300)),
     "heads_200": dict(B=2, Hq=200, Hkv=200, T=2, C=1, S=2, prefix=(0, 300)),
@@ -294,7 +299,7 @@ def test_pages_outside_the_pool_read_as_zeros_and_a_malformed_tree_as_a_status(g
 
 
 @pytest.mark.parametrize("kw", [dict(T=6, C=2, S=20, prefix=[250, 60, 126]), dict(T=6, C=2, S=0, D=64, Hq=4, prefix=[250, 60, 126]),
-                                dict(T=8, C=4, S=3, Hq=4, Hkv=2, prefix=[250, 60, 126]), dict(T=40, C=20, S=40, prefix=[250, 60, 126]),
+                                dict(T=8, C=4, S=3, Hq=4, Hkv=2, prefix=[250, 60, 126]), dict(T=8, C=4, S=3, Hq=4, Hkv=2, D=64, prefix=[250, 60, 126]), dict(T=40, C=20, S=40, prefix=[250, 60, 126]),
                                 dict(B=40, T=40, C=20, S=5, prefix=(0, 300), Hkv=4, Hq=16), dict(B=40, T=40, C=20, S=5, prefix=(0, 300), Hkv=4, Hq=16, D=64)])
 def test_values_that_are_not_numbers_reach_the_rows_that_see_them_alone(gpu, kw):
     """NaN codes in keys and values of tree slots and soft prompts, a column of a value each: exactly the rows that see them, exactly that column."""
