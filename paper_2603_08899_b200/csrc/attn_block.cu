@@ -139,9 +139,9 @@ __device__ void fetch_role(Sh& sh, int ring, const Params& prm, const BlockParam
         // (soft prompts have scales like a page's; -1: outside the pool, or no such chunk)
         auto page_of = [&](int j) -> int { return j < ch.n_keys ? __ldg(table + s.t0 + (j >> 2)) : j < ch.n ? 0 : -1; };
         auto scales_of = [&](int j, int page) -> float2 {
-            if ((uint32_t)page >= (uint64_t)bp.n_pages) return make_float2(1.f, 1.f);
-            const size_t at = ((size_t)page * prm.d.Hkv + s.g) * nb + ch.sub(j) * kChunk / bp.block;
             const bool soft = j >= ch.n_keys;
+            if (soft ? j >= ch.n : (uint32_t)page >= (uint64_t)bp.n_pages) return make_float2(1.f, 1.f);
+            const size_t at = ((size_t)page * prm.d.Hkv + s.g) * nb + ch.sub(j) * kChunk / bp.block;
             return make_float2(__ldg((soft ? bp.ks_soft : bp.ks) + at), __ldg((soft ? bp.vs_soft : bp.vs) + at));
         };
         int j = (ring + Sh::kWarps - (int)(i0 % Sh::kWarps)) % Sh::kWarps;
@@ -179,7 +179,8 @@ __device__ __forceinline__ void fetch_ahead(int ring, const Params& prm, const B
     const int4* w = reinterpret_cast<const int4*>(pv.cta + blockIdx.x);
     const int4 w0 = __ldcg(w), w1 = __ldcg(w + 1);
     const int b = w0.x, g = prm.kind == kPlanHeads ? w0.y >> 16 : w0.y & 0xffff, t = w0.z + (ring >> 2);
-    if (b < 0 || b >= prm.d.B || g < 0 || g >= prm.d.Hkv || w0.z < 0 || t >= w0.w || t >= w1.x - (prm.d.S > 0 ? 1 : 0) || t >= prm.map.max_pages) return;
+    // (t < 0: the sum has left the integers)
+    if (b < 0 || b >= prm.d.B || g < 0 || g >= prm.d.Hkv || w0.z < 0 || t < 0 || t >= w0.w || t >= w1.x - (prm.d.S > 0 ? 1 : 0) || t >= prm.map.max_pages) return;
     const int page = __ldcg(prm.map.block_table + (size_t)b * prm.map.max_pages + t);
     if ((uint32_t)page >= (uint64_t)bp.n_pages) return;
     tma_prefetch_3d(k_map, 0, g, page * kTileKeys + (ring & 3) * kChunk);

@@ -212,6 +212,27 @@ def test_a_plan_for_the_other_kernel_is_refused(gpu, kw):
         assert (out == 7.0).all() and (lse == 7.0).all()
 
 
+@pytest.mark.parametrize("T,C", [(1, 0), (3, 1), (30, 10)])
+def test_a_plan_that_is_written_while_the_attention_is_on_its_way(gpu, T, C):
+    """What is fetched ahead by the plan buffer's old contents is a hint, whatever they are."""
+    case = Case(seed=46, T=T, C=C, S=0 if C == 0 else 4)
+    d = case.device()
+    dims = case.dims()
+    want = attend(gpu, case, d)
+    plan = torch.empty(cb.confu_plan_bytes(gpu.ctx, dims) // 4 + 1, dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros_like(d["q"]), torch.zeros(case.B, case.R, case.Hq, device="cuda")
+    status = torch.zeros(case.B, dtype=torch.int32, device="cuda")
+    for fill in (-1, 0, 1, 0x7FFFFFFF, 0x7FFFFFFE, -2 ** 31):
+        for _ in range(4):
+            plan.fill_(fill)
+            cb.confu_tree_plan(gpu.ctx, dims, None, d["P"], d["parent"], d["owner"], plan, status)
+            cb.confu_tree_attention(gpu.ctx, dims, d["q"], d["k"], d["v"], case.n_pages * PAGE, None, d["P"], d["k_soft"], d["v_soft"], None, None, plan, out, lse,
+                                    status)
+        torch.cuda.synchronize()
+        assert (status == 0).all()
+        assert np.array_equal(out.double().cpu().numpy(), want[0]) and np.array_equal(lse.double().cpu().numpy(), want[1])
+
+
 @pytest.mark.parametrize("T,C", [(3, 1), (30, 10)])
 def test_entries_behind_four_gigabytes(gpu, T, C):
     """A pool of which the last pages alone are in use, past 2^32 bytes: append, attention, compaction and copies give what a small pool gives."""
