@@ -452,9 +452,18 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_empty);
 
-        // ---- the end of a run: the warps meet, 4 or 16 rows at a time ----
+        // ---- the end of a run: the warps meet, 4 or 16 rows at a time; at the end of the CTA's last run all at once, in their rings, which nothing fills any
+        // more (one sequence of 2048, 16 rows: a launch 14.7 us, LASTUS so) ----
         constexpr int kVec = D / 4;                  // float4s of a row
         const bool whole = s.part_slot < 0;
+        const bool small = w.left > 1 || n_rows <= Sh::kRowsAtOnce;
+        const int at_once = small ? Sh::kRowsAtOnce : kMt * 16;
+        static_assert(kMt * 16 * (Sh::kPitch * sizeof(float) + sizeof(float2)) <= sizeof(sh.kv[0]), "sums in a ring");
+        constexpr int kRing = sizeof(sh.kv[0]) / sizeof(float);
+        float* const sums = small ? &sh.sums[0][0][0] : reinterpret_cast<float*>(sh.kv);                             // [warp][row]
+        const int sums_step = small ? Sh::kRowsAtOnce * Sh::kPitch : kRing;
+        float2* const stats = small ? &sh.stat[0][0] : reinterpret_cast<float2*>(sums + kMt * 16 * Sh::kPitch);      // [warp][row]
+        const int stats_step = small ? Sh::kRowsAtOnce : kRing / 2;
 #pragma unroll
         for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
@@ -462,41 +471,39 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
                 l[mt][o] += __shfl_xor_sync(0xffffffffu, l[mt][o], 1);
                 l[mt][o] += __shfl_xor_sync(0xffffffffu, l[mt][o], 2);
             }
-#pragma unroll
-        for (int pass = 0; pass < kMt * 16 / Sh::kRowsAtOnce; ++pass) {
-            const int row0 = pass * Sh::kRowsAtOnce;
-            if (row0 >= n_rows) break;
+#pragma unroll 1
+        for (int row0 = 0; row0 < n_rows; row0 += at_once) {
+            const int here = min(n_rows - row0, at_once);
             // (what the warps wrote the last time they met has been read by all of them)
             if (n_met > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sh.met, (n_met - 1) & 1, &sh.abort, prm.wait_ns)) && ok;
 #pragma unroll
-            for (int q = 0; q < kMt; ++q) {
-                // one M tile: rows 4 pass .. 4 pass + 3, of the lanes with n / 4 = pass % 2; two: the 16 rows of M tile `pass`
-                const int mt = kMt == 1 ? 0 : pass, o = kMt == 1 ? pass / 2 : q;
-                const int row = kMt == 1 ? n & 3 : n + 8 * q;                 // of this pass
-                if (row0 + row < n_rows && (kMt == 2 || n / 4 == pass % 2)) {
-                    if (x == 0) sh.stat[warp][row] = make_float2(m_ref[mt][o], l[mt][o]);
-                    // columns n' of a product's tile u: head dim n' * D / 8 + u; the lane's two columns are 2 x and 2 x + 1: D / 4 contiguous head dims
-                    float* to = &sh.sums[warp][row][x * Sh::kSeg];
+            for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
-                    for (int u = 0; u < D / 4; u += 4) {
-                        const int c = u < D / 8 ? 2 * o : 2 * o + 1, v = u % (D / 8);
-                        *reinterpret_cast<float4*>(to + u) = make_float4(o_acc[mt][v][c], o_acc[mt][v + 1][c], o_acc[mt][v + 2][c], o_acc[mt][v + 3][c]);
+                for (int o = 0; o < 2; ++o) {
+                    const int row = mt * 16 + n + 8 * o - row0;
+                    if ((uint32_t)row < (uint32_t)here) {
+                        if (x == 0) stats[warp * stats_step + row] = make_float2(m_ref[mt][o], l[mt][o]);
+                        // columns n' of a product's tile u: head dim n' * D / 8 + u; the lane's two columns are 2 x and 2 x + 1: D / 4 contiguous head dims
+                        float* to = sums + warp * sums_step + row * Sh::kPitch + x * Sh::kSeg;
+#pragma unroll
+                        for (int u = 0; u < D / 4; u += 4) {
+                            const int c = u < D / 8 ? 2 * o : 2 * o + 1, v = u % (D / 8);
+                            *reinterpret_cast<float4*>(to + u) = make_float4(o_acc[mt][v][c], o_acc[mt][v + 1][c], o_acc[mt][v + 2][c], o_acc[mt][v + 3][c]);
+                        }
                     }
                 }
-            }
             sync();
-            const int here = min(n_rows - row0, Sh::kRowsAtOnce);
             for (int e = threadIdx.x; e < here * kVec; e += Sh::kWarps * 32) {
                 const int row = e / kVec, v = e % kVec, m = row0 + row;
                 float M = -INFINITY, L = 0.f;
 #pragma unroll
-                for (int k = 0; k < Sh::kWarps; ++k) M = fmaxf(M, sh.stat[k][row].x);
+                for (int k = 0; k < Sh::kWarps; ++k) M = fmaxf(M, stats[k * stats_step + row].x);
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
                 for (int k = 0; k < Sh::kWarps; ++k) {
-                    const float2 ml = sh.stat[k][row];
+                    const float2 ml = stats[k * stats_step + row];
                     const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-                    const float4 y = *reinterpret_cast<const float4*>(&sh.sums[k][row][(v / (kVec / 4)) * Sh::kSeg + (v % (kVec / 4)) * 4]);
+                    const float4 y = *reinterpret_cast<const float4*>(sums + k * sums_step + row * Sh::kPitch + (v / (kVec / 4)) * Sh::kSeg + (v % (kVec / 4)) * 4);
                     L = fmaf(f, ml.y, L);
                     acc.x = fmaf(f, y.x, acc.x);
                     acc.y = fmaf(f, y.y, acc.y);
