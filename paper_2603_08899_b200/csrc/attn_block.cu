@@ -26,6 +26,8 @@
 #include "e4m3.cuh"
 #include "tc_walk.cuh"
 
+#include <type_traits>
+
 namespace confu {
 namespace tc {
 
@@ -456,14 +458,6 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
         // more (one sequence of 2048, 16 rows: a launch 14.7 us, LASTUS so) ----
         constexpr int kVec = D / 4;                  // float4s of a row
         const bool whole = s.part_slot < 0;
-        const bool small = w.left > 1 || n_rows <= Sh::kRowsAtOnce;
-        const int at_once = small ? Sh::kRowsAtOnce : kMt * 16;
-        static_assert(kMt * 16 * (Sh::kPitch * sizeof(float) + sizeof(float2)) <= sizeof(sh.kv[0]), "sums in a ring");
-        constexpr int kRing = sizeof(sh.kv[0]) / sizeof(float);
-        float* const sums = small ? &sh.sums[0][0][0] : reinterpret_cast<float*>(sh.kv);                             // [warp][row]
-        const int sums_step = small ? Sh::kRowsAtOnce * Sh::kPitch : kRing;
-        float2* const stats = small ? &sh.stat[0][0] : reinterpret_cast<float2*>(sums + kMt * 16 * Sh::kPitch);      // [warp][row]
-        const int stats_step = small ? Sh::kRowsAtOnce : kRing / 2;
 #pragma unroll
         for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
@@ -471,6 +465,13 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
                 l[mt][o] += __shfl_xor_sync(0xffffffffu, l[mt][o], 1);
                 l[mt][o] += __shfl_xor_sync(0xffffffffu, l[mt][o], 2);
             }
+        auto meet = [&](auto in_rings) {
+        constexpr bool kAll = decltype(in_rings)::value;
+        constexpr int at_once = kAll ? kMt * 16 : Sh::kRowsAtOnce;
+        static_assert(kMt * 16 * (Sh::kPitch * sizeof(float) + sizeof(float2)) <= sizeof(sh.kv[0]), "sums in a ring");
+        constexpr int kRing = sizeof(sh.kv[0]) / sizeof(float), sums_step = kAll ? kRing : Sh::kRowsAtOnce * Sh::kPitch, stats_step = kAll ? kRing / 2 : Sh::kRowsAtOnce;
+        float* const sums = kAll ? reinterpret_cast<float*>(sh.kv) : &sh.sums[0][0][0];                             // [warp][row]
+        float2* const stats = kAll ? reinterpret_cast<float2*>(sums + kMt * 16 * Sh::kPitch) : &sh.stat[0][0];      // [warp][row]
 #pragma unroll 1
         for (int row0 = 0; row0 < n_rows; row0 += at_once) {
             const int here = min(n_rows - row0, at_once);
@@ -551,6 +552,9 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
             if (lane == 0) mbar_arrive(&sh.met);
             ++n_met;
         }
+        };
+        if (w.left > 1 || n_rows <= Sh::kRowsAtOnce) meet(std::false_type{});
+        else meet(std::true_type{});
         i0 += (uint32_t)ch.n;
         run = next_run(w, prm, s);
     }
