@@ -455,7 +455,7 @@ __device__ void consumer_role(Sh& sh, const Params& prm, const BlockParams& bp, 
         if (lane == 0) mbar_arrive(&sh.q_empty);
 
         // ---- the end of a run: the warps meet, 4 or 16 rows at a time; at the end of the CTA's last run all at once, in their rings, which nothing fills any
-        // more (one sequence of 2048, 16 rows: a launch 14.7 us, LASTUS so) ----
+        // more (one sequence of 4096, 16 rows: a layer 16.4 us, 13.4 so) ----
         constexpr int kVec = D / 4;                  // float4s of a row
         const bool whole = s.part_slot < 0;
 #pragma unroll
@@ -633,7 +633,7 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const Params& prm, const BlockP
 
 // Rows x heads of a kv head: one M tile of 16, two at D = 64, whose fragments are half as many.  From there on the tcgen05 kernel is faster, whose time
 // hardly depends on the rows (us, graph; this kernel / that one; one sequence of 4096 x 4 layers, 16 of 500..4000 x 2, 64 of 100..4000 x 2;
-// 8 kv heads).  D = 128: 4 rows 45 / 64, 51 / 91, 132 / 248; 16 rows 66 / 66, 82 / 92, 171 / 250; 20 rows, with two M tiles, 70 / 66, 95 / 94,
+// 8 kv heads).  D = 128: 4 rows 45 / 64, 51 / 91, 132 / 248; 16 rows 53 / 66, 73 / 92, 165 / 250; 20 rows, with two M tiles, 70 / 66, 95 / 94,
 // 249 / 251; 32 rows 78 / 66, 107 / 95, 267 / 253.  D = 64: 4 rows 39 / 53, 39 / 70; 32 rows 53 / 53, 61 / 70.
 bool block_register_supported(const confu_dims& d) { return (d.T + d.C) * (d.Hq / d.Hkv) <= (d.D == 64 ? 32 : 16); }
 
