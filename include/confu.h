@@ -405,7 +405,8 @@ typedef struct {
 size_t confu_pages_workspace_bytes(int32_t n_pages);
 
 /* Row rows[i] gets the pages that it lacks for lengths[i] slots: ceil(lengths[i] / 128) entries (a step's rows count: prefix + R).  A row named
- * twice is refused (CONFU_ST_BAD_PAGES) the second time. */
+ * twice is refused (CONFU_ST_BAD_PAGES) the second time.  A row whose request is refused still lacks the entries: a step that needs them is not to be run
+ * (confu_set_paging asks for valid ids). */
 int confu_pages_reserve(confu_ctx* ctx, const confu_pages* pages, int32_t n, const int32_t* rows, const int32_t* lengths,
                         int32_t* status, void* stream);
 

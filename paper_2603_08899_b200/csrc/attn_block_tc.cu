@@ -974,7 +974,9 @@ cudaError_t launch(const CUtensorMap (&maps)[3], const Params& prm, const BlockP
 }  // namespace tc
 
 // Whether a CTA works on one M tile, its two warpgroups on half of the keys of every tile each: where one holds the rows, and where (sequence, kv
-// head, M tile) triples are few for the SMs, as for a bf16 cache.
+// head, M tile) triples are few for the SMs, as for a bf16 cache.  (Against two M tiles, us, graph: one sequence of 4096, 64 rows of 4 heads, four
+// layers 82 -> 76; head dim 64, four of 1500..2500 103 -> 92; seven of 37..5001, 48 rows x heads in one tile, 117 -> 111.  Where triples are many the
+// second tile shares the first one's codes and their conversion: 32 of 512..16384 are 320 a layer that way.)
 bool block_one_tile(const confu_dims& d, int sm_count)
 {
     const int n_tiles = row_groups(d.T + d.C, d.Hq / d.Hkv, 1);
